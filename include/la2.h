@@ -446,6 +446,110 @@ void la2_set_chunk_tokens(int32_t tokens);
  */
 void la2_set_scan_variant(int32_t variant);
 
+/*
+ * The operators of a decoder layer around the recurrence, and those of a program that generates with it.
+ *
+ * Conventions are those above (device pointers, caller's stream and workspace, errors before any launch, nothing allocated, nothing kept),
+ * with these differences: matrices are [rows, features] with one element stride between rows, which may be any that is at
+ * least the number of features (base pointers stay 16-byte aligned; rows that are whole 16-byte pieces are the fast case), sizes
+ * may be any.  Weights, biases, row statistics and the gradients of weight and bias of the normalisation, the bias and
+ * its gradient of the linear layer, and scores are fp32 whatever the dtype.  Sums are fp32 or wider, each output is rounded once.
+ *
+ * Layer normalisation over the features of each row:
+ *     y = (x - mean) rstd weight + bias,   rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   x, y, dy, dx   [rows, width] of dtype, `stride` elements between rows (all the same)
+ *   weight, bias   fp32 [width], or NULL for 1 and 0
+ *   mean, rstd     fp32 [rows], written by the forward pass and read by the backward pass
+ *   d_weight, d_bias  fp32 [width], or NULL if not wanted (they do not depend on weight or bias being given)
+ * y may be x, dx may be dy.  The backward pass sums the rows of d_weight and d_bias in a fixed order, through the workspace:
+ * la2_layer_norm_workspace_bytes() bytes, 256-byte aligned, not needed (NULL) if both are NULL.  No rows: d_weight and d_bias
+ * are set to 0.  eps as for la2_fwd_norm (LA2_ERR_VALUE).
+ */
+size_t la2_layer_norm_workspace_bytes(int64_t rows, int32_t width, int32_t dtype);
+la2_status la2_layer_norm_fwd(int64_t rows, int32_t width, int32_t dtype, int64_t stride, const void* x,
+                              const float* weight, const float* bias, float eps, void* y, float* mean,
+                              float* rstd, void* hip_stream);
+la2_status la2_layer_norm_bwd(int64_t rows, int32_t width, int32_t dtype, int64_t stride, const void* x,
+                              const void* dy, const float* weight, const float* mean, const float* rstd,
+                              void* dx, float* d_weight, float* d_bias, void* workspace,
+                              size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Linear layer with its epilogue, and its gradients:
+ *     z = x w^T + bias,   y = act(z) + residual
+ *     dz = dy act'(z),   dx = dz w,   dw = dz^T x,   d_bias = sum over rows of dz      (the residual's gradient is dy)
+ * act: none, max(z, 0) (slope 0 at 0), z Phi(z) with the normal distribution function Phi, z / (1 + exp(-z)).
+ */
+typedef enum { LA2_ACT_NONE = 0, LA2_ACT_RELU = 1, LA2_ACT_GELU = 2, LA2_ACT_SILU = 3 } la2_act;
+
+/* Host-side description: x, dx [rows, in_features]; w, dw [out_features, in_features]; y, pre, residual, dy [rows, out_features]. */
+typedef struct {
+  int64_t rows;
+  int32_t in_features;
+  int32_t out_features;
+  int32_t dtype;    /* la2_dtype of all matrices */
+  int32_t act;      /* la2_act; another value: LA2_ERR_VALUE */
+  int64_t stride_x; /* elements between rows of x and dx            */
+  int64_t stride_w; /*                          w and dw            */
+  int64_t stride_y; /*                          y, pre, residual, dy */
+} la2_linear_desc;
+
+/*
+ * Bytes of workspace of la2_linear_fwd (op LA2_OP_FWD) or la2_linear_bwd (LA2_OP_BWD, all outputs wanted); 0 for an invalid
+ * descriptor.  It holds copies of operands whose rows are no whole 16-byte pieces, the sums of products whose reduction is cut,
+ * dz, and the rows' shares of d_bias.  Depends on the device's compute-unit count.  256-byte aligned; may be NULL when 0.
+ */
+size_t la2_linear_workspace_bytes(const la2_linear_desc* desc, int32_t op);
+
+/*
+ *   bias      fp32 [out_features] or NULL;  residual  or NULL
+ *   pre       out  z (rounded to dtype), for the backward pass, or NULL if not wanted
+ * y may be residual.  Rows of at most 2^23 - 1 bytes, at most 2^40 elements per matrix (LA2_ERR_SHAPE).
+ * fp32 data: products and sums in fp32 (the fp32 matrix instructions).
+ */
+la2_status la2_linear_fwd(const la2_linear_desc* desc, const void* x, const void* w, const float* bias,
+                          const void* residual, void* y, void* pre, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+/*
+ *   pre       z as the forward pass left it; may be NULL for LA2_ACT_NONE
+ *   dx, dw, d_bias  out, NULL where not wanted (x is then not needed for dw, w not for dx)
+ * dz is rounded to dtype for the two products (16-bit data), d_bias is formed from the unrounded values.  No rows: dw and d_bias are 0.
+ */
+la2_status la2_linear_bwd(const la2_linear_desc* desc, const void* x, const void* w, const void* pre,
+                          const void* dy, void* dx, void* dw, float* d_bias, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/*
+ * One step of beam search, per batch row: of the candidates (beam i, token t) with the score
+ *     scores[i] + log_softmax(logits[i])[t]
+ * the `beams` best, the best first, equal ones in the order of beam, then token.  A finished beam has one candidate, its own
+ * score with token eos.  A beam whose score is -inf or NaN has none (first step: scores 0, -inf, -inf, ...), nor
+ * has a token whose logit is -inf (masked) or NaN; a logit of +inf counts as the largest finite value.  Slots that are left over when there are
+ * too few candidates get score -inf, their own index as parent, token eos (0 without one) and are finished.
+ *   logits    [batch, beams, vocab] of dtype, stride_row elements between rows (of a beam; batch rows follow at beams * stride_row)
+ *   scores    fp32 [batch, beams];  finished  [batch, beams] bytes, non-zero: finished; or NULL for none (then eos may be -1)
+ *   eos       the token that finishes a beam, -1: none (LA2_ERR_VALUE outside -1 .. vocab - 1, or -1 with `finished`)
+ *   out_scores, parent, token, out_finished   [batch, beams]: fp32, int32, int32, bytes (0 or 1); out_scores may be scores,
+ *             out_finished may be finished
+ *   workspace la2_beam_select_workspace_bytes(), 256-byte aligned
+ * 1 <= beams <= 32, 1 <= vocab <= 2^20, batch * beams <= 65535 (LA2_ERR_SHAPE).  Scores are ranked in 64 bits and rounded once.
+ */
+size_t la2_beam_select_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t dtype);
+la2_status la2_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t dtype, int64_t stride_row,
+                           const void* logits, const float* scores, const uint8_t* finished, int32_t eos,
+                           float* out_scores, int32_t* parent, int32_t* token, uint8_t* out_finished,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The states that move with the beams, in place: states[s][b][i] <- states[s][b][parent[b][i]] for nstates buffers (the layers'
+ * decode states, say), each dense [batch, beams, row_bytes], as one launch per 64 of them.
+ *   states    HOST array of nstates device pointers, 16-byte aligned;  row_bytes  a multiple of 16 (LA2_ERR_STRIDE_ALIGN)
+ *   parent    int32 [batch, beams]; a value outside 0 .. beams - 1 leaves its beam as it is
+ * 1 <= beams <= 32, batch <= 65535 (LA2_ERR_SHAPE).  A beam that is its own parent is neither read nor written.
+ */
+la2_status la2_beam_reorder(int32_t nstates, void* const* states, int32_t batch, int32_t beams, int64_t row_bytes,
+                            const int32_t* parent, void* hip_stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* la2_status_string(la2_status status);
 

@@ -38,6 +38,14 @@ class la2_desc(ctypes.Structure):
     ]
 
 
+class la2_linear_desc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+        ("stride_x", ctypes.c_int64), ("stride_w", ctypes.c_int64), ("stride_y", ctypes.c_int64),
+    ]
+
+
 def lib_path():
     return _LIB_PATH
 
@@ -112,6 +120,26 @@ def load():
     lib.la2_decode_multi.restype = ctypes.c_int
     lib.la2_decode_step.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.la2_decode_step.restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.la2_layer_norm_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.la2_layer_norm_workspace_bytes.restype = sz
+    lib.la2_layer_norm_fwd.argtypes = [i64, i32, i32, i64, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
+    lib.la2_layer_norm_fwd.restype = ctypes.c_int
+    lib.la2_layer_norm_bwd.argtypes = [i64, i32, i32, i64] + [vp] * 9 + [sz, vp]
+    lib.la2_layer_norm_bwd.restype = ctypes.c_int
+    ldp = ctypes.POINTER(la2_linear_desc)
+    lib.la2_linear_workspace_bytes.argtypes = [ldp, i32]
+    lib.la2_linear_workspace_bytes.restype = sz
+    lib.la2_linear_fwd.argtypes = [ldp] + [vp] * 7 + [sz, vp]
+    lib.la2_linear_fwd.restype = ctypes.c_int
+    lib.la2_linear_bwd.argtypes = [ldp] + [vp] * 8 + [sz, vp]
+    lib.la2_linear_bwd.restype = ctypes.c_int
+    lib.la2_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.la2_beam_select_workspace_bytes.restype = sz
+    lib.la2_beam_select.argtypes = [i32, i32, i32, i32, i64, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.la2_beam_select.restype = ctypes.c_int
+    lib.la2_beam_reorder.argtypes = [i32, ctypes.POINTER(vp), i32, i32, i64, vp, vp]
+    lib.la2_beam_reorder.restype = ctypes.c_int
     lib.la2_status_string.argtypes = [ctypes.c_int]
     lib.la2_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -604,3 +632,76 @@ def la2_left_product_bwd(q, k, v, d_o, lam, out=None):
     dq, dk, dv = _outputs(lib, q, out)
     _run(lib.la2_left_product_bwd, q, q, q, k, v, d_o, lam, dq, dk, dv)
     return dq, dk, dv
+
+
+# ---- the operators around the recurrence
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _act(name):
+    try:
+        return _ACTS[name]
+    except (KeyError, TypeError):
+        raise ValueError("la2: act must be one of %s, got %r" % (", ".join(sorted(_ACTS)), name)) from None
+
+
+def _call(entry, t, *args):
+    """entry(*args, stream) of the native module on the current stream of t's device, which is made the current device; its outputs."""
+    device = t.get_device()
+    if device == _current_device():
+        out = entry(*args, _current_stream(device))
+    else:
+        with torch.cuda.device(device):
+            out = entry(*args, _current_stream(device))
+    if type(out) is int:
+        _check(out)
+    return out
+
+
+def la2_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, mean=None, rstd=None):
+    """(y, mean, rstd): every row of x ([..., features], bf16, fp16 or fp32) brought to mean 0 and deviation 1, times weight, plus bias
+    (fp32 [features] or None).  mean, rstd (fp32, x's leading dimensions) are what la2_layer_norm_bwd takes."""
+    lib = _module()
+    _on_gpu(x, "la2_layer_norm_fwd")
+    return _call(lib.layer_norm_fwd, x, x, weight, bias, eps, out, mean, rstd)
+
+
+def la2_layer_norm_bwd(dy, x, mean, rstd, weight=None, want_d_weight=True, want_d_bias=True, out=None, workspace=None):
+    """(dx, d_weight, d_bias) of sum(la2_layer_norm_fwd(x, weight, bias)[0] * dy); d_weight, d_bias fp32, None where not wanted."""
+    lib = _module()
+    _on_gpu(x, "la2_layer_norm_bwd")
+    return _call(lib.layer_norm_bwd, x, dy, x, mean, rstd, weight, want_d_weight, want_d_bias, out, workspace)
+
+
+def la2_linear_fwd(x, w, bias=None, residual=None, act="none", want_pre=False, out=None, pre=None, workspace=None):
+    """(y, pre): y = act(x w^T + bias) + residual for x [..., in_features], w [out_features, in_features], bias fp32 or None, residual like y or
+    None, act "none", "relu", "gelu" or "silu".  pre (want_pre, or the caller's tensor): the sums in front of the
+    activation, which la2_linear_bwd takes; else None."""
+    lib = _module()
+    _on_gpu(x, "la2_linear_fwd")
+    return _call(lib.linear_fwd, x, x, w, bias, residual, _act(act), want_pre, out, pre, workspace)
+
+
+def la2_linear_bwd(dy, x, w, pre=None, act="none", want_dx=True, want_dw=True, want_d_bias=True, workspace=None):
+    """(dx, dw, d_bias) of sum(la2_linear_fwd(x, w, bias, act=act)[0] * dy), None for what is not wanted; pre: the forward call's, not needed
+    for act "none".  d_bias is fp32.  (The gradient of a residual is dy.)"""
+    lib = _module()
+    _on_gpu(x, "la2_linear_bwd")
+    return _call(lib.linear_bwd, x, dy, x, w, pre, _act(act), want_dx, want_dw, want_d_bias, workspace)
+
+
+def la2_beam_select(logits, scores, finished=None, eos=-1, workspace=None):
+    """One step of beam search: (scores, parent, token, finished), each [batch, beams], of the `beams` best continuations of every batch row,
+    the best first.  logits [batch, beams, vocab], scores fp32, finished bool or None, eos the token that finishes a beam (-1: none)."""
+    lib = _module()
+    _on_gpu(logits, "la2_beam_select")
+    return _call(lib.beam_select, logits, logits, scores, finished, eos, workspace)
+
+
+def la2_beam_reorder(states, parent):
+    """Moves the beams' states to where la2_beam_select's parent (int32 [batch, beams]) wants them, in place: row b * beams + i of every tensor
+    in `states` (one, or a sequence of equal ones, such as the decode states of all layers) becomes its row b * beams + parent[b, i]."""
+    lib = _module()
+    _on_gpu(parent, "la2_beam_reorder")
+    _call(lib.beam_reorder, parent, [states] if isinstance(states, torch.Tensor) else states, parent)
+    return states

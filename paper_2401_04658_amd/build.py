@@ -12,7 +12,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libla2.so")
 SOURCES = ["la2_api.hip", "la2_scan_bf16.hip", "la2_scan_bf16_half.hip", "la2_bwd_scans_bf16.hip", "la2_chunk_state_bf16.hip",
            "la2_left_product_bf16.hip", "la2_scan_f32.hip", "la2_decode.hip", "la2_recur.hip", "la2_norm.hip", "la2_tail_bf16.hip", "la2_scan_wide.hip",
-           "la2_short_bf16.hip"]
+           "la2_short_bf16.hip", "la2_layer_api.hip", "la2_layer_norm.hip", "la2_linear.hip", "la2_linear_bf16.hip", "la2_linear_f16.hip",
+           "la2_linear_f32.hip", "la2_beam.hip"]
 BENCH_LIB = os.path.join(_HERE, "libla2_bench.so")
 BENCH_SOURCES = ["bench_probe.hip"]
 NATIVE = os.path.join(_HERE, "_la2_native.so")

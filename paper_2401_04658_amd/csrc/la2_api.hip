@@ -939,6 +939,10 @@ la2::RecurParams recur_params(const la2_desc* d, const float* lambda, int t0, in
 
 }  // namespace
 
+namespace la2 {
+int device_units() { return device_cu_count(); }
+}  // namespace la2
+
 extern "C" {
 
 void la2_desc_dense(la2_desc* desc, int32_t batch, int32_t heads, int32_t seqlen, int32_t head_dim,

@@ -7,6 +7,8 @@
 
 namespace la2 {
 
+int device_units();   // compute units of the current device (la2_api.hip)
+
 // element types of the sequence tensors (the values of la2_dtype)
 enum { kF32 = 0, kBF16 = 1, kF16 = 2 };
 

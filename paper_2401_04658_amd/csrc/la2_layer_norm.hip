@@ -1,0 +1,354 @@
+// Layer normalisation over the features of a row, forward and backward.
+//
+//   mean = sum_j x_j / W,  rstd = 1 / sqrt(sum_j (x_j - mean)^2 / W + eps),  h = (x - mean) rstd,  y = h w + b
+//   g = dy w,  dx = rstd (g - sum_j g_j / W - h sum_j g_j h_j / W),  dw = sum_rows dy h,  db = sum_rows dy
+//
+// Bound by memory: a row is read once and stays in registers (CH pieces of 16 bytes per lane, TPR lanes a row), so the variance
+// is taken around the mean that was just formed.  A group of lanes walks over rows with w, b and, backward, its columns' share of
+// dw and db in registers; sums are fp32.  The shares meet in LDS, then in `partial`, which a second launch sums column by column in
+// a fixed order: no atomics, the same bits in every run.
+#include "la2_layer.h"
+
+namespace la2 {
+namespace {
+
+template <int TPR>
+struct Shape {
+  static constexpr int kThreads = TPR > 256 ? TPR : 256;
+  static constexpr int kRows = kThreads / TPR;   // rows that a workgroup works on at a time
+};
+
+// Sums of a row over its TPR lanes, in every lane.  `red`: one entry per wave; the caller uses two in turn, so that one barrier per
+// sum is enough.
+template <int TPR>
+__device__ __forceinline__ float2 row_sum(float a, float b, float2* red) {
+#pragma unroll
+  for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1) {
+    a += __shfl_xor(a, m);
+    b += __shfl_xor(b, m);
+  }
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; w++) {
+      a += red[w].x;
+      b += red[w].y;
+    }
+  }
+  return make_float2(a, b);
+}
+
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(LayerNormParams p) {
+  constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
+  __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float w[CH][N], b[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; c++)
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int j = (c * TPR + lane) * N + i;
+      w[c][i] = p.weight != nullptr && j < p.width ? p.weight[j] : 1.f;
+      b[c][i] = p.bias != nullptr && j < p.width ? p.bias[j] : 0.f;
+    }
+  const float width = (float)p.width;   // divided by, so that the mean of equal numbers is that number
+  for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB) {
+    const T* x = static_cast<const T*>(p.x) + row * p.stride;
+    float v[CH][N], s = 0.f, q = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      Piece<T>::load(x, (c * TPR + lane) * N, p.width, v[c]);
+#pragma unroll
+      for (int i = 0; i < N; i++) s += v[c][i];
+    }
+    const float mean = row_sum<TPR>(s, 0.f, red[0]).x / width;
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        v[c][i] -= mean;
+        if ((c * TPR + lane) * N + i < p.width) q = fmaf(v[c][i], v[c][i], q);
+      }
+    const float rstd = 1.f / sqrtf(row_sum<TPR>(q, 0.f, red[1]).x / width + p.eps);
+    T* y = static_cast<T*>(p.y) + row * p.stride;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+#pragma unroll
+      for (int i = 0; i < N; i++) v[c][i] = fmaf(v[c][i] * rstd, w[c][i], b[c][i]);
+      Piece<T>::store(y, (c * TPR + lane) * N, p.width, v[c]);
+    }
+    if (lane == 0) {
+      p.mean[row] = mean;
+      p.rstd[row] = rstd;
+    }
+  }
+}
+
+// TPR lanes, the columns' sums of dw (x) and db (y) of a workgroup's rows: to d_weight / d_bias where it is the only workgroup, else
+// to its row of partial
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(LayerNormParams p) {
+  constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
+  __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
+  __shared__ float2 share[RPB > 1 ? TPR * CH * N : 1];
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float w[CH][N], aw[CH][N], ab[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; c++)
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int j = (c * TPR + lane) * N + i;
+      w[c][i] = p.weight != nullptr && j < p.width ? p.weight[j] : 1.f;
+      aw[c][i] = ab[c][i] = 0.f;
+    }
+  const float width = (float)p.width;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
+    const T* x = static_cast<const T*>(p.x) + row * p.stride;
+    const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float h[CH][N], g[CH][N], sg = 0.f, sh = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      Piece<T>::load(x, (c * TPR + lane) * N, p.width, h[c]);
+      Piece<T>::load(dy, (c * TPR + lane) * N, p.width, g[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+      for (int i = 0; i < N; i++) {   // behind the row's end g is 0, so that whatever h is there adds nothing
+        h[c][i] = (c * TPR + lane) * N + i < p.width ? (h[c][i] - mean) * rstd : 0.f;
+        aw[c][i] = fmaf(g[c][i], h[c][i], aw[c][i]);
+        ab[c][i] += g[c][i];
+        g[c][i] *= w[c][i];
+        sg += g[c][i];
+        sh = fmaf(g[c][i], h[c][i], sh);
+      }
+    const float2 s = row_sum<TPR>(sg, sh, red[turn]);
+    const float mg = s.x / width, mh = s.y / width;
+    T* dx = static_cast<T*>(p.y) + row * p.stride;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+#pragma unroll
+      for (int i = 0; i < N; i++) g[c][i] = rstd * (g[c][i] - mg - h[c][i] * mh);
+      Piece<T>::store(dx, (c * TPR + lane) * N, p.width, g[c]);
+    }
+  }
+  if (p.d_weight == nullptr && p.d_bias == nullptr) return;
+  if constexpr (RPB > 1) {
+    for (int r = 0; r < RPB; r++) {
+      if (sub == r) {
+#pragma unroll
+        for (int c = 0; c < CH; c++)
+#pragma unroll
+          for (int i = 0; i < N; i++) {
+            float2& at = share[(c * N + i) * TPR + lane];
+            if (r > 0) {
+              aw[c][i] += at.x;
+              ab[c][i] += at.y;
+            }
+            if (r < RPB - 1) at = make_float2(aw[c][i], ab[c][i]);
+          }
+      }
+      __syncthreads();
+    }
+    if (sub != RPB - 1) return;
+  }
+  const bool only = gridDim.x == 1;
+  float* ow = only ? p.d_weight : p.partial + (int64_t)blockIdx.x * 2 * p.width;
+  float* ob = only ? p.d_bias : p.partial + ((int64_t)blockIdx.x * 2 + 1) * p.width;
+#pragma unroll
+  for (int c = 0; c < CH; c++)
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int j = (c * TPR + lane) * N + i;
+      if (j >= p.width) continue;
+      if (ow != nullptr) ow[j] = aw[c][i];
+      if (ob != nullptr) ob[j] = ab[c][i];
+    }
+}
+
+// Rows that no group of lanes holds in registers: they are read again for every pass over them, from the caches.
+constexpr int kWideThreads = 1024;
+template <typename T>
+__global__ __launch_bounds__(kWideThreads) void layer_norm_wide_fwd_kernel(LayerNormParams p) {
+  __shared__ float2 red[2][kWideThreads / 64];
+  const float width = (float)p.width;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T* x = static_cast<const T*>(p.x) + row * p.stride;
+    float s = 0.f, q = 0.f;
+    for (int j = threadIdx.x; j < p.width; j += kWideThreads) s += (float)x[j];
+    const float mean = row_sum<kWideThreads>(s, 0.f, red[0]).x / width;
+    for (int j = threadIdx.x; j < p.width; j += kWideThreads) q = fmaf((float)x[j] - mean, (float)x[j] - mean, q);
+    const float rstd = 1.f / sqrtf(row_sum<kWideThreads>(q, 0.f, red[1]).x / width + p.eps);
+    T* y = static_cast<T*>(p.y) + row * p.stride;
+    for (int j = threadIdx.x; j < p.width; j += kWideThreads)
+      y[j] = (T)fmaf(((float)x[j] - mean) * rstd, p.weight != nullptr ? p.weight[j] : 1.f, p.bias != nullptr ? p.bias[j] : 0.f);
+    if (threadIdx.x == 0) {
+      p.mean[row] = mean;
+      p.rstd[row] = rstd;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kWideThreads) void layer_norm_wide_bwd_kernel(LayerNormParams p) {
+  __shared__ float2 red[2][kWideThreads / 64];
+  const float width = (float)p.width;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    const T* x = static_cast<const T*>(p.x) + row * p.stride;
+    const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float sg = 0.f, sh = 0.f;
+    for (int j = threadIdx.x; j < p.width; j += kWideThreads) {
+      const float g = (float)dy[j] * (p.weight != nullptr ? p.weight[j] : 1.f);
+      sg += g;
+      sh = fmaf(g, ((float)x[j] - mean) * rstd, sh);
+    }
+    const float2 s = row_sum<kWideThreads>(sg, sh, red[turn]);
+    T* dx = static_cast<T*>(p.y) + row * p.stride;
+    for (int j = threadIdx.x; j < p.width; j += kWideThreads) {
+      const float g = (float)dy[j] * (p.weight != nullptr ? p.weight[j] : 1.f);
+      dx[j] = (T)(rstd * (g - s.x / width - ((float)x[j] - mean) * rstd * (s.y / width)));
+    }
+  }
+}
+
+// ... and their columns' sums: workgroup (x, y) sums 256 columns over every gridDim.y-th row
+template <typename T>
+__global__ __launch_bounds__(256) void layer_norm_wide_columns_kernel(LayerNormParams p) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= p.width) return;
+  float aw = 0.f, ab = 0.f;
+  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+    const float g = (float)static_cast<const T*>(p.dy)[row * p.stride + j];
+    aw = fmaf(g, ((float)static_cast<const T*>(p.x)[row * p.stride + j] - p.mean[row]) * p.rstd[row], aw);
+    ab += g;
+  }
+  p.partial[(int64_t)blockIdx.y * 2 * p.width + j] = aw;
+  p.partial[((int64_t)blockIdx.y * 2 + 1) * p.width + j] = ab;
+}
+
+// d_weight, d_bias = the sums over `count` rows of partial: 16 columns a workgroup, 16 threads each
+__global__ __launch_bounds__(256) void layer_norm_sum_kernel(const float* partial, int64_t count, int32_t width, float* d_weight,
+                                                             float* d_bias) {
+  __shared__ float part[16][16 + 1];
+  const int col = threadIdx.x % 16, slice = threadIdx.x / 16;
+  const int64_t j = (int64_t)blockIdx.x * 16 + col, all = 2 * (int64_t)width;
+  float a = 0.f;
+  if (j < all) {
+#pragma unroll 8
+    for (int64_t r = slice; r < count; r += 16) a += partial[r * all + j];
+  }
+  part[slice][col] = a;
+  __syncthreads();
+  if (slice != 0 || j >= all) return;
+  a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; i++) a += part[i][col];
+  if (j < width) {
+    if (d_weight != nullptr) d_weight[j] = a;
+  } else if (d_bias != nullptr) {
+    d_bias[j - width] = a;
+  }
+}
+
+template <int TPR, int CH>
+struct Split {
+  static constexpr int tpr = TPR, ch = CH;
+};
+// Calls f(Split) for the lanes and pieces of a row of `width`, f(Split<0, 0>) where no split holds it.
+template <typename T, bool BWD, typename F>
+auto split_of(int32_t width, F f) {
+  const int pieces = (width + Piece<T>::N - 1) / Piece<T>::N;
+  if (pieces <= 8) return f(Split<8, 1>{});
+  if (pieces <= 16) return f(Split<16, 1>{});
+  if (pieces <= 32) return f(Split<32, 1>{});
+  if (pieces <= 64) return f(Split<64, 1>{});
+  if (pieces <= 128) return f(Split<64, 2>{});
+  if constexpr (!BWD)
+    if (pieces <= 256) return f(Split<64, 4>{});
+  if (pieces <= 256) return f(Split<256, 1>{});
+  if (pieces <= 512) return f(Split<256, 2>{});
+  if (pieces <= 1024) return f(Split<256, 4>{});
+  if (pieces <= 2048) return f(Split<1024, 2>{});
+  return f(Split<0, 0>{});
+}
+
+// Workgroups of a pass: as many as hold all rows, at most `most` per unit
+template <int TPR>
+int64_t groups(int64_t rows, int units, int most) {
+  const int64_t need = (rows + Shape<TPR>::kRows - 1) / Shape<TPR>::kRows;
+  const int64_t fit = (int64_t)units * (TPR > 256 ? 2 : most);
+  return need < 1 ? 1 : need < fit ? need : fit;   // no rows: one, which sets the gradients to 0
+}
+constexpr int kFwdPerUnit = 8, kBwdPerUnit = 4;
+
+template <typename T>
+hipError_t fwd(const LayerNormParams& p, int units, hipStream_t s) {
+  return split_of<T, false>(p.width, [&](auto split) {
+    using S = decltype(split);
+    if constexpr (S::tpr == 0)
+      hipLaunchKernelGGL(layer_norm_wide_fwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
+    else
+      hipLaunchKernelGGL((layer_norm_fwd_kernel<T, S::tpr, S::ch>), dim3((unsigned)groups<S::tpr>(p.rows, units, kFwdPerUnit)),
+                         dim3(Shape<S::tpr>::kThreads), 0, s, p);
+    return hipGetLastError();
+  });
+}
+
+template <typename T>
+int64_t partials(int64_t rows, int32_t width, int units) {
+  return split_of<T, true>(width, [&](auto split) -> int64_t {
+    using S = decltype(split);
+    if constexpr (S::tpr == 0) return rows < 1 ? 1 : rows < 64 ? rows : 64;
+    const int64_t g = groups<S::tpr == 0 ? 64 : S::tpr>(rows, units, kBwdPerUnit);
+    return g > 1 ? g : 0;
+  });
+}
+
+template <typename T>
+hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
+  const bool sums = p.d_weight != nullptr || p.d_bias != nullptr;
+  const int64_t count = partials<T>(p.rows, p.width, units);
+  hipError_t e = split_of<T, true>(p.width, [&](auto split) {
+    using S = decltype(split);
+    if constexpr (S::tpr == 0) {
+      if (sums)   // first: dx may take dy's place
+        hipLaunchKernelGGL(layer_norm_wide_columns_kernel<T>, dim3((unsigned)((p.width + 255) / 256), (unsigned)count), dim3(256), 0, s, p);
+      hipLaunchKernelGGL(layer_norm_wide_bwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
+    } else {
+      hipLaunchKernelGGL((layer_norm_bwd_kernel<T, S::tpr, S::ch>), dim3((unsigned)groups<S::tpr>(p.rows, units, kBwdPerUnit)),
+                         dim3(Shape<S::tpr>::kThreads), 0, s, p);
+    }
+    return hipGetLastError();
+  });
+  if (e != hipSuccess || !sums || count == 0) return e;
+  hipLaunchKernelGGL(layer_norm_sum_kernel, dim3((unsigned)((2 * (int64_t)p.width + 15) / 16)), dim3(256), 0, s, p.partial, count, p.width,
+                     p.d_weight, p.d_bias);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm_fwd(int dtype, const LayerNormParams& p, int units, hipStream_t s) {
+  if (dtype == kBF16) return fwd<__bf16>(p, units, s);
+  if (dtype == kF16) return fwd<_Float16>(p, units, s);
+  return fwd<float>(p, units, s);
+}
+
+hipError_t launch_layer_norm_bwd(int dtype, const LayerNormParams& p, int units, hipStream_t s) {
+  if (dtype == kBF16) return bwd<__bf16>(p, units, s);
+  if (dtype == kF16) return bwd<_Float16>(p, units, s);
+  return bwd<float>(p, units, s);
+}
+
+int64_t layer_norm_bwd_partials(int dtype, int64_t rows, int32_t width, int units) {
+  return dtype == kF32 ? partials<float>(rows, width, units) : partials<__bf16>(rows, width, units);
+}
+
+}  // namespace la2

@@ -14,6 +14,7 @@
 #include <exception>
 #include <tuple>
 #include <utility>
+#include <vector>
 
 #include "../../include/la2.h"
 
@@ -293,6 +294,300 @@ PyObject* decode_shape(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- the operators around the recurrence: checks, output tensors and the call.  Each answers with a tuple of outputs, or with the
+// status (a number) of a refused call.
+struct Rows {   // a tensor as rows of features
+  int64_t rows = 1, width = 1, stride = 1;
+};
+Rows rows_of(const at::Tensor& t, const char* what) {
+  Rows r;
+  const int64_t dims = t.dim();
+  if (dims < 1 || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) {
+    PyErr_Format(PyExc_ValueError, "la2: %s must have contiguous features", what);
+    throw Raised{};
+  }
+  r.width = t.size(dims - 1);
+  r.stride = r.width;
+  int64_t next = 0;   // stride that the dimension in front of those seen has to have; 0: any
+  for (int64_t d = dims - 2; d >= 0; d--) {
+    const int64_t n = t.size(d);
+    r.rows *= n;
+    if (n == 1) continue;
+    if (next == 0) r.stride = t.stride(d);
+    else if (t.stride(d) != next) {
+      PyErr_Format(PyExc_ValueError, "la2: %s must be rows at one distance", what);
+      throw Raised{};
+    }
+    next = t.stride(d) * n;
+  }
+  return r;
+}
+void same_rows(const at::Tensor& t, const at::Tensor& ref, const char* what) {
+  if (t.sizes() != ref.sizes() || t.strides() != ref.strides() || t.scalar_type() != ref.scalar_type() || t.device() != ref.device()) {
+    PyErr_Format(PyExc_ValueError, "la2: %s: another shape, layout, dtype or device than expected", what);
+    throw Raised{};
+  }
+}
+// o, where it is a contiguous tensor of this type and these sizes on ref's device
+const at::Tensor& dense(PyObject* o, const at::Tensor& ref, at::ScalarType type, at::IntArrayRef sizes, const char* what) {
+  const at::Tensor& t = tensor(o);
+  if (t.sizes() != sizes || t.scalar_type() != type || t.device() != ref.device() || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "la2: %s: another shape, dtype or device than expected, or not contiguous", what);
+    throw Raised{};
+  }
+  return t;
+}
+at::Tensor fresh(at::IntArrayRef sizes, const at::Tensor& ref, at::ScalarType type) {
+  return at::empty(sizes, at::TensorOptions().dtype(type).device(ref.device()));
+}
+at::Tensor as(const at::Tensor& t) { return at::empty_strided(t.sizes(), t.strides(), at::TensorOptions().dtype(t.dtype()).device(t.device())); }
+// The caller's tensor (dense() of it), or a new one
+at::Tensor dense_or_new(PyObject* o, const at::Tensor& ref, at::ScalarType type, at::IntArrayRef sizes, const char* what) {
+  return o == Py_None ? fresh(sizes, ref, type) : dense(o, ref, type, sizes, what);
+}
+at::Tensor same_or_new(PyObject* o, const at::Tensor& ref, const char* what) {
+  if (o == Py_None) return as(ref);
+  same_rows(tensor(o), ref, what);
+  return tensor(o);
+}
+// Data of an optional dense vector
+template <typename T>
+const T* dense_or_null(PyObject* o, const at::Tensor& ref, at::ScalarType type, at::IntArrayRef sizes, const char* what) {
+  return o == Py_None ? nullptr : static_cast<const T*>(dense(o, ref, type, sizes, what).data_ptr());
+}
+// The caller's workspace or a new one of `need` bytes (undefined for none)
+at::Tensor workspace_of(PyObject* o, const at::Tensor& ref, size_t need) {
+  if (o != Py_None) {
+    if (tensor(o).device() != ref.device()) raise(PyExc_ValueError, "la2: the workspace is on another device");
+    return tensor(o);
+  }
+  return need == 0 ? at::Tensor() : fresh({(int64_t)need}, ref, at::kByte);
+}
+void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+size_t bytes(const at::Tensor& t) { return t.defined() ? (size_t)t.numel() * t.element_size() : 0; }
+PyObject* wrap(const at::Tensor& t) {
+  if (!t.defined()) Py_RETURN_NONE;
+  return THPVariable_Wrap(t);
+}
+template <typename... T>
+PyObject* answer(la2_status st, const T&... t) {
+  if (st != LA2_OK) return PyLong_FromLong((long)st);
+  PyObject* const out = PyTuple_New(sizeof...(T));
+  if (out == nullptr) return nullptr;
+  Py_ssize_t i = 0;
+  const bool fine = ([&] {
+    PyObject* const o = wrap(t);
+    if (o == nullptr) return false;
+    PyTuple_SET_ITEM(out, i++, o);
+    return true;
+  }() && ...);
+  if (fine) return out;
+  Py_DECREF(out);
+  return nullptr;
+}
+template <typename F>
+la2_status unlocked(F f) {
+  la2_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f();
+  Py_END_ALLOW_THREADS
+  return st;
+}
+bool truth(PyObject* o) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) throw Raised{};
+  return t != 0;
+}
+void expects(Py_ssize_t n, Py_ssize_t want) {
+  if (n == want) return;
+  PyErr_Format(PyExc_TypeError, "la2: %zd arguments, not %zd", want, n);
+  throw Raised{};
+}
+
+// layer_norm_fwd(x, weight, bias, eps, out, mean, rstd, stream): (y, mean, rstd)
+PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 8);
+    const at::Tensor& x = tensor(a[0]);
+    const Rows r = rows_of(x, "x");
+    const int dtype = dtype_code(x);
+    const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+    const float* const weight = dense_or_null<float>(a[1], x, at::kFloat, {r.width}, "weight");
+    const float* const bias = dense_or_null<float>(a[2], x, at::kFloat, {r.width}, "bias");
+    const float eps = Arg<float>(a[3]).get();
+    const at::Tensor y = same_or_new(a[4], x, "out"), mean = dense_or_new(a[5], x, at::kFloat, lead, "mean"),
+                     rstd = dense_or_new(a[6], x, at::kFloat, lead, "rstd");
+    void* const stream = Arg<void*>(a[7]).get();
+    return answer(unlocked([&] {
+      return la2_layer_norm_fwd(r.rows, extent(r.width), dtype, r.stride, x.data_ptr(), weight, bias, eps, y.data_ptr(),
+                                static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), stream);
+    }), y, mean, rstd);
+  });
+}
+
+// layer_norm_bwd(dy, x, mean, rstd, weight, want_d_weight, want_d_bias, out, workspace, stream): (dx, d_weight, d_bias)
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 10);
+    const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]);
+    const Rows r = rows_of(x, "x");
+    const int dtype = dtype_code(x);
+    same_rows(dy, x, "dy");
+    const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+    const float* const mean = static_cast<const float*>(dense(a[2], x, at::kFloat, lead, "mean").data_ptr());
+    const float* const rstd = static_cast<const float*>(dense(a[3], x, at::kFloat, lead, "rstd").data_ptr());
+    const float* const weight = dense_or_null<float>(a[4], x, at::kFloat, {r.width}, "weight");
+    at::Tensor dw, db;
+    if (truth(a[5])) dw = fresh({r.width}, x, at::kFloat);
+    if (truth(a[6])) db = fresh({r.width}, x, at::kFloat);
+    const at::Tensor dx = same_or_new(a[7], x, "out");
+    const int32_t width = extent(r.width);
+    const at::Tensor ws = workspace_of(a[8], x, dw.defined() || db.defined() ? la2_layer_norm_workspace_bytes(r.rows, width, dtype) : 0);
+    void* const stream = Arg<void*>(a[9]).get();
+    return answer(unlocked([&] {
+      return la2_layer_norm_bwd(r.rows, width, dtype, r.stride, x.data_ptr(), dy.data_ptr(), weight, mean, rstd, dx.data_ptr(),
+                                static_cast<float*>(data(dw)), static_cast<float*>(data(db)), data(ws), bytes(ws), stream);
+    }), dx, dw, db);
+  });
+}
+
+la2_linear_desc linear_desc(const at::Tensor& x, const at::Tensor& w, PyObject* act) {
+  la2_linear_desc d{};
+  const Rows rx = rows_of(x, "x"), rw = rows_of(w, "w");
+  if (w.dim() != 2 || rw.width != rx.width) raise(PyExc_ValueError, "la2: w must be [out_features, in_features] of x's features");
+  if (w.scalar_type() != x.scalar_type() || w.device() != x.device()) raise(PyExc_ValueError, "la2: x and w must share dtype and device");
+  d.rows = rx.rows;
+  d.in_features = extent(rx.width);
+  d.out_features = extent(rw.rows);
+  d.dtype = dtype_code(x);
+  d.act = Integer<int32_t>(act).get();
+  d.stride_x = rx.stride;
+  d.stride_w = rw.stride;
+  return d;
+}
+void of_output(const at::Tensor& t, const at::Tensor& x, const la2_linear_desc& d, const char* what) {
+  if (t.dim() != x.dim() || t.sizes().slice(0, x.dim() - 1) != x.sizes().slice(0, x.dim() - 1) || t.size(x.dim() - 1) != d.out_features ||
+      t.scalar_type() != x.scalar_type() || t.device() != x.device()) {
+    PyErr_Format(PyExc_ValueError, "la2: %s must be x's rows of out_features, x's dtype and device", what);
+    throw Raised{};
+  }
+}
+
+// linear_fwd(x, w, bias, residual, act, want_pre, out, pre, workspace, stream): (y, pre or None)
+PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 10);
+    const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
+    la2_linear_desc d = linear_desc(x, w, a[4]);
+    const float* const bias = dense_or_null<float>(a[2], x, at::kFloat, {d.out_features}, "bias");
+    at::Tensor y, pre;
+    const void* residual = nullptr;
+    if (a[3] != Py_None) {
+      of_output(tensor(a[3]), x, d, "residual");
+      residual = tensor(a[3]).data_ptr();
+      y = same_or_new(a[6], tensor(a[3]), "out");
+    } else if (a[6] != Py_None) {
+      of_output(tensor(a[6]), x, d, "out");
+      y = tensor(a[6]);
+    } else {
+      at::DimVector sizes(x.sizes().begin(), x.sizes().end());
+      sizes[sizes.size() - 1] = d.out_features;
+      y = fresh(sizes, x, x.scalar_type());
+    }
+    d.stride_y = rows_of(y, "out").stride;
+    if (a[7] != Py_None || truth(a[5])) pre = same_or_new(a[7], y, "pre");
+    const at::Tensor ws = workspace_of(a[8], x, la2_linear_workspace_bytes(&d, LA2_OP_FWD));
+    void* const stream = Arg<void*>(a[9]).get();
+    return answer(unlocked([&] {
+      return la2_linear_fwd(&d, x.data_ptr(), w.data_ptr(), bias, residual, y.data_ptr(), data(pre), data(ws), bytes(ws), stream);
+    }), y, pre);
+  });
+}
+
+// linear_bwd(dy, x, w, pre, act, want_dx, want_dw, want_d_bias, workspace, stream): (dx, dw, d_bias), None for what is not wanted
+PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 10);
+    const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]), &w = tensor(a[2]);
+    la2_linear_desc d = linear_desc(x, w, a[4]);
+    of_output(dy, x, d, "dy");
+    d.stride_y = rows_of(dy, "dy").stride;
+    const void* pre = nullptr;
+    if (a[3] != Py_None) {
+      same_rows(tensor(a[3]), dy, "pre");
+      pre = tensor(a[3]).data_ptr();
+    }
+    at::Tensor dx, dw, db;
+    if (truth(a[5])) dx = as(x);
+    if (truth(a[6])) dw = as(w);
+    if (truth(a[7])) db = fresh({d.out_features}, x, at::kFloat);
+    const at::Tensor ws = workspace_of(a[8], x, la2_linear_workspace_bytes(&d, LA2_OP_BWD));
+    void* const stream = Arg<void*>(a[9]).get();
+    return answer(unlocked([&] {
+      return la2_linear_bwd(&d, x.data_ptr(), w.data_ptr(), pre, dy.data_ptr(), data(dx), data(dw), static_cast<float*>(data(db)), data(ws),
+                            bytes(ws), stream);
+    }), dx, dw, db);
+  });
+}
+
+// beam_select(logits, scores, finished, eos, workspace, stream): (scores, parent, token, finished)
+PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 6);
+    const at::Tensor& logits = tensor(a[0]);
+    if (logits.dim() != 3) raise(PyExc_ValueError, "la2: logits must be [batch, beams, vocab]");
+    const Rows r = rows_of(logits, "logits");
+    const int dtype = dtype_code(logits);
+    const int32_t batch = extent(logits.size(0)), beams = extent(logits.size(1)), vocab = extent(r.width);
+    const at::IntArrayRef lead = logits.sizes().slice(0, 2);
+    const float* const scores = static_cast<const float*>(dense(a[1], logits, at::kFloat, lead, "scores").data_ptr());
+    const uint8_t* const finished = dense_or_null<uint8_t>(a[2], logits, at::kBool, lead, "finished");
+    const int32_t eos = Integer<int32_t>(a[3]).get();
+    const at::Tensor ws = workspace_of(a[4], logits, la2_beam_select_workspace_bytes(batch, beams, vocab, dtype));
+    const at::Tensor out = fresh(lead, logits, at::kFloat), parent = fresh(lead, logits, at::kInt), token = fresh(lead, logits, at::kInt),
+                     done = fresh(lead, logits, at::kBool);
+    void* const stream = Arg<void*>(a[5]).get();
+    return answer(unlocked([&] {
+      return la2_beam_select(batch, beams, vocab, dtype, r.stride, logits.data_ptr(), scores, finished, eos, static_cast<float*>(out.data_ptr()),
+                             static_cast<int32_t*>(parent.data_ptr()), static_cast<int32_t*>(token.data_ptr()),
+                             static_cast<uint8_t*>(done.data_ptr()), data(ws), bytes(ws), stream);
+    }), out, parent, token, done);
+  });
+}
+
+// beam_reorder(states (a sequence of tensors), parent, stream): the status
+PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expects(n, 3);
+    const at::Tensor& parent = tensor(a[1]);
+    if (parent.dim() != 2 || parent.scalar_type() != at::kInt || !parent.is_contiguous())
+      raise(PyExc_ValueError, "la2: parent must be contiguous int32 [batch, beams]");
+    const int32_t batch = extent(parent.size(0)), beams = extent(parent.size(1));
+    PyObject* const seq = PySequence_Fast(a[0], "la2: states must be tensors");
+    if (seq == nullptr) throw Raised{};
+    struct Release {
+      PyObject* o;
+      ~Release() { Py_DECREF(o); }
+    } release{seq};
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
+    std::vector<void*> at((size_t)count);
+    int64_t row = 0;
+    for (Py_ssize_t i = 0; i < count; i++) {
+      const at::Tensor& s = tensor(PySequence_Fast_GET_ITEM(seq, i));
+      if (s.dim() < 1 || s.size(0) != (int64_t)batch * beams || !s.is_contiguous() || s.device() != parent.device())
+        raise(PyExc_ValueError, "la2: states must be contiguous, one for each of batch * beams, on parent's device");
+      const int64_t size = s.size(0) == 0 ? 0 : s.numel() / s.size(0) * (int64_t)s.element_size();
+      if (i > 0 && size != row) raise(PyExc_ValueError, "la2: states must be of one size");
+      row = size;
+      at[(size_t)i] = s.data_ptr();
+    }
+    void* const stream = Arg<void*>(a[2]).get();
+    const int32_t states = extent(count);
+    const int32_t* const from = static_cast<const int32_t*>(parent.data_ptr());
+    return PyLong_FromLong((long)unlocked([&] { return la2_beam_reorder(states, at.data(), batch, beams, row, from, stream); }));
+  });
+}
+
 #define FAST(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 #define ENTRY(f) FAST(#f, (&Entry<f>::call))
 PyMethodDef methods[] = {
@@ -302,7 +597,8 @@ PyMethodDef methods[] = {
     ENTRY(la2_decode_step), ENTRY(la2_decode_step_norm), ENTRY(la2_decode_multi), ENTRY(la2_decode_multi_norm),
     ENTRY(la2_left_product_fwd), ENTRY(la2_left_product_bwd),
     FAST("same_layout", same_layout), FAST("given", given), FAST("f32", f32), FAST("workspace", workspace), FAST("state", state),
-    FAST("decode_shape", decode_shape),
+    FAST("decode_shape", decode_shape), FAST("layer_norm_fwd", layer_norm_fwd), FAST("layer_norm_bwd", layer_norm_bwd),
+    FAST("linear_fwd", linear_fwd), FAST("linear_bwd", linear_bwd), FAST("beam_select", beam_select), FAST("beam_reorder", beam_reorder),
     {"like", like, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 #undef ENTRY
