@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "la2_internal.h"
 
 namespace la2 {
@@ -18,16 +20,30 @@ struct Piece {
   typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
   typedef vec at_element __attribute__((aligned(sizeof(T))));
 
-  // elements at .. at + N - 1 of a row of `width` elements, 0 behind its end
-  static __device__ __forceinline__ void load(const T* row, int at, int width, float (&v)[N]) {
-    if (at + N <= width) {
-      const vec u = *reinterpret_cast<const at_element*>(row + at);
-#pragma unroll
-      for (int i = 0; i < N; i++) v[i] = (float)u[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; i++) v[i] = at + i < width ? (float)row[at + i] : 0.f;
+  // elements at .. at + N - 1 (at a multiple of N) of a row of `width` elements, 0 behind its end: there the row's last N elements, moved
+  // down (one load instead of up to N)
+  static __device__ __forceinline__ vec raw(const T* row, int64_t at, int64_t width) {
+    typedef unsigned __int128 bits;
+    if (at + N <= width) return *reinterpret_cast<const at_element*>(row + at);
+    bits u = 0;
+    if (at < width) {
+      if (width >= N) {
+        const vec last = *reinterpret_cast<const at_element*>(row + width - N);
+        u = __builtin_bit_cast(bits, last) >> (8 * (int)sizeof(T) * (int)(at + N - width));
+      } else {
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < (int)width; i++) {
+          typedef std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t> word;
+          u |= (bits)reinterpret_cast<const word*>(row)[i] << (8 * (int)sizeof(T) * i);
+        }
+      }
     }
+    return __builtin_bit_cast(vec, u);
+  }
+  static __device__ __forceinline__ void load(const T* row, int at, int width, float (&v)[N]) {
+    const vec u = raw(row, at, width);
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = (float)u[i];
   }
   static __device__ __forceinline__ void store(T* row, int at, int width, const float (&v)[N]) {
     if (at + N <= width) {
@@ -42,6 +58,32 @@ struct Piece {
     }
   }
 };
+
+// A value that the compiler takes for new: what was formed from the old one is formed again rather than kept in registers.
+template <typename T>
+__device__ __forceinline__ T renewed(T x) {
+  if constexpr (std::is_integral_v<T>) asm volatile("" : "+s"(x));
+  else asm volatile("" : "+v"(x));
+  return x;
+}
+
+// N floats of a vector of `width` from element `at` (a multiple of 4) on, `other` behind its end and for a vector that is not given.  The
+// vector starts at a multiple of 16 bytes.
+template <int N>
+__device__ __forceinline__ void load_floats(const float* p, int64_t at, int64_t width, float other, float (&v)[N]) {
+  typedef __attribute__((ext_vector_type(4))) float f4;
+  if (p != nullptr && at + N <= width) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const f4 u = *reinterpret_cast<const f4*>(p + at + i);
+#pragma unroll
+      for (int k = 0; k < 4; k++) v[i + k] = u[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = p != nullptr && at + i < width ? p[at + i] : other;
+  }
+}
 
 struct LayerNormParams {
   int64_t rows;
@@ -73,7 +115,7 @@ struct BeamSelectParams {
   const float* scores;        // [batch][beams]
   const uint8_t* finished;    // [batch][beams] or nullptr
   int32_t eos;                // -1: none
-  int32_t chunks;             // pieces of the vocabulary
+  int32_t chunks, parts;      // workgroups of a row, and parts of the vocabulary that each works off
   uint64_t* keys;             // workspace: [batch * beams][chunks][beams]
   float2* sums;               // workspace: [batch * beams][chunks] (largest logit, sum of exp against it)
   float* out_scores;
@@ -81,8 +123,8 @@ struct BeamSelectParams {
   int32_t* token;
   uint8_t* out_finished;
 };
-int beam_select_chunks(int dtype, int64_t rows, int32_t vocab, int units);
-hipError_t launch_beam_select(int dtype, const BeamSelectParams& p, hipStream_t s);
+int beam_select_chunks(int64_t rows, int32_t beams, int32_t vocab, int units);
+hipError_t launch_beam_select(int dtype, BeamSelectParams p, int units, hipStream_t s);   // sets chunks and parts
 
 constexpr int kMaxStatesPerLaunch = 64;
 struct BeamReorderParams {

@@ -193,7 +193,7 @@ la2_status la2_linear_bwd(const la2_linear_desc* desc, const void* x, const void
 size_t la2_beam_select_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t dtype) {
   if (check_select(batch, beams, vocab, dtype) != LA2_OK) return 0;
   const int64_t rows = (int64_t)batch * beams;
-  const int chunks = la2::beam_select_chunks(dtype, rows, vocab, la2::device_units());
+  const int chunks = la2::beam_select_chunks(rows, beams, vocab, la2::device_units());
   return select_sums(rows, chunks) + (size_t)rows * chunks * beams * sizeof(uint64_t);
 }
 
@@ -218,14 +218,14 @@ la2_status la2_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t 
   p.scores = scores;
   p.finished = finished;
   p.eos = eos;
-  p.chunks = la2::beam_select_chunks(dtype, (int64_t)batch * beams, vocab, la2::device_units());
+  const int units = la2::device_units();
   p.sums = static_cast<float2*>(workspace);
-  p.keys = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + select_sums((int64_t)batch * beams, p.chunks));
+  p.keys = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + select_sums((int64_t)batch * beams, la2::beam_select_chunks((int64_t)batch * beams, beams, vocab, units)));
   p.out_scores = out_scores;
   p.parent = parent;
   p.token = token;
   p.out_finished = out_finished;
-  return launched(la2::launch_beam_select(dtype, p, reinterpret_cast<hipStream_t>(hip_stream)));
+  return launched(la2::launch_beam_select(dtype, p, units, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 la2_status la2_beam_reorder(int32_t nstates, void* const* states, int32_t batch, int32_t beams, int64_t row_bytes, const int32_t* parent,

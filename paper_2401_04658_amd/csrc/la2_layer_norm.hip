@@ -47,38 +47,46 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float w[CH][N], b[CH][N];
 #pragma unroll
-  for (int c = 0; c < CH; c++)
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      const int j = (c * TPR + lane) * N + i;
-      w[c][i] = p.weight != nullptr && j < p.width ? p.weight[j] : 1.f;
-      b[c][i] = p.bias != nullptr && j < p.width ? p.bias[j] : 0.f;
-    }
+  for (int c = 0; c < CH; c++) {
+    load_floats(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
+    load_floats(p.bias, (c * TPR + lane) * N, p.width, 0.f, b[c]);
+  }
   const float width = (float)p.width;   // divided by, so that the mean of equal numbers is that number
   for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
+    const int end = renewed(p.width);   // the masks of a ragged end are formed for every row: kept, they overflow the scalar registers
     float v[CH][N], s = 0.f, q = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      Piece<T>::load(x, (c * TPR + lane) * N, p.width, v[c]);
+      Piece<T>::load(x, (c * TPR + lane) * N, end, v[c]);
 #pragma unroll
       for (int i = 0; i < N; i++) s += v[c][i];
     }
     const float mean = row_sum<TPR>(s, 0.f, red[0]).x / width;
 #pragma unroll
-    for (int c = 0; c < CH; c++)
+    for (int c = 0; c < CH; c++) {
+      const int at = (c * TPR + lane) * N;
+      if (at + N <= end) {
 #pragma unroll
-      for (int i = 0; i < N; i++) {
-        v[c][i] -= mean;
-        if ((c * TPR + lane) * N + i < p.width) q = fmaf(v[c][i], v[c][i], q);
+        for (int i = 0; i < N; i++) {
+          v[c][i] -= mean;
+          q = fmaf(v[c][i], v[c][i], q);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+          v[c][i] = at + i < end ? v[c][i] - mean : 0.f;
+          q = fmaf(v[c][i], v[c][i], q);
+        }
       }
+    }
     const float rstd = 1.f / sqrtf(row_sum<TPR>(q, 0.f, red[1]).x / width + p.eps);
     T* y = static_cast<T*>(p.y) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
 #pragma unroll
       for (int i = 0; i < N; i++) v[c][i] = fmaf(v[c][i] * rstd, w[c][i], b[c][i]);
-      Piece<T>::store(y, (c * TPR + lane) * N, p.width, v[c]);
+      Piece<T>::store(y, (c * TPR + lane) * N, end, v[c]);
     }
     if (lane == 0) {
       p.mean[row] = mean;
@@ -95,46 +103,54 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
   __shared__ float2 share[RPB > 1 ? TPR * CH * N : 1];
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  constexpr bool KEEP = CH * N <= 16;   // the weights stay in registers; else they come from the caches, twice a row
   float w[CH][N], aw[CH][N], ab[CH][N];
 #pragma unroll
-  for (int c = 0; c < CH; c++)
+  for (int c = 0; c < CH; c++) {
+    if (KEEP) load_floats(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      const int j = (c * TPR + lane) * N + i;
-      w[c][i] = p.weight != nullptr && j < p.width ? p.weight[j] : 1.f;
-      aw[c][i] = ab[c][i] = 0.f;
-    }
+    for (int i = 0; i < N; i++) aw[c][i] = ab[c][i] = 0.f;
+  }
   const float width = (float)p.width;
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
     const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
     const float mean = p.mean[row], rstd = p.rstd[row];
-    float h[CH][N], g[CH][N], sg = 0.f, sh = 0.f;
+    const int end = renewed(p.width);
+    typename Piece<T>::vec rx[CH], rg[CH];   // the row as it is stored: h and g are formed twice rather than kept
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      Piece<T>::load(x, (c * TPR + lane) * N, p.width, h[c]);
-      Piece<T>::load(dy, (c * TPR + lane) * N, p.width, g[c]);
+      rx[c] = Piece<T>::raw(x, (c * TPR + lane) * N, end);
+      rg[c] = Piece<T>::raw(dy, (c * TPR + lane) * N, end);
     }
+    float sg = 0.f, sh = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; c++)
+    for (int c = 0; c < CH; c++) {
+      if (!KEEP) load_floats(p.weight, (c * TPR + lane) * N, end, 1.f, w[c]);
 #pragma unroll
-      for (int i = 0; i < N; i++) {   // behind the row's end g is 0, so that whatever h is there adds nothing
-        h[c][i] = (c * TPR + lane) * N + i < p.width ? (h[c][i] - mean) * rstd : 0.f;
-        aw[c][i] = fmaf(g[c][i], h[c][i], aw[c][i]);
-        ab[c][i] += g[c][i];
-        g[c][i] *= w[c][i];
-        sg += g[c][i];
-        sh = fmaf(g[c][i], h[c][i], sh);
+      for (int i = 0; i < N; i++) {   // behind the row's end dy is 0, and h finite in a row that is
+        const float h = ((float)rx[c][i] - mean) * rstd, d = (float)rg[c][i], g = d * w[c][i];
+        aw[c][i] = fmaf(d, h, aw[c][i]);
+        ab[c][i] += d;
+        sg += g;
+        sh = fmaf(g, h, sh);
       }
+    }
     const float2 s = row_sum<TPR>(sg, sh, red[turn]);
     const float mg = s.x / width, mh = s.y / width;
     T* dx = static_cast<T*>(p.y) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
+      if (CH > 1) {
+        rx[c] = renewed(rx[c]);
+        rg[c] = renewed(rg[c]);
+      }
+      if (!KEEP) load_floats(p.weight, (c * TPR + lane) * N, renewed(end), 1.f, w[c]);
+      float v[N];
 #pragma unroll
-      for (int i = 0; i < N; i++) g[c][i] = rstd * (g[c][i] - mg - h[c][i] * mh);
-      Piece<T>::store(dx, (c * TPR + lane) * N, p.width, g[c]);
+      for (int i = 0; i < N; i++) v[i] = rstd * ((float)rg[c][i] * w[c][i] - mg - ((float)rx[c][i] - mean) * rstd * mh);
+      Piece<T>::store(dx, (c * TPR + lane) * N, end, v);
     }
   }
   if (p.d_weight == nullptr && p.d_bias == nullptr) return;
@@ -274,8 +290,10 @@ auto split_of(int32_t width, F f) {
     if (pieces <= 256) return f(Split<64, 4>{});
   if (pieces <= 256) return f(Split<256, 1>{});
   if (pieces <= 512) return f(Split<256, 2>{});
-  if (pieces <= 1024) return f(Split<256, 4>{});
-  if (pieces <= 2048) return f(Split<1024, 2>{});
+  if (pieces <= 1024) return f(Split<512, 2>{});
+  if constexpr (BWD && sizeof(T) == 2)   // 32 elements a lane do not fit the registers beside their sums
+    if (pieces <= 2048) return f(Split<1024, 2>{});
+  if (pieces <= 2048) return f(Split<512, 4>{});
   return f(Split<0, 0>{});
 }
 

@@ -109,25 +109,25 @@ __device__ __forceinline__ float act_slope(float z, int act) {
 template <typename E, int N>
 __device__ __forceinline__ void finish(const ProductParams& p, int64_t i, int64_t j, float (&v)[N]) {
   static_assert(N == Piece<E>::N, "one piece");
-  const int left = (int)min(p.J - j, (int64_t)N);
-  const int64_t at = i * p.ldo + j;
+  const int64_t row = i * p.ldo;
   if (p.bias != nullptr) {
+    float b[N];
+    load_floats(p.bias, j, p.J, 0.f, b);
 #pragma unroll
-    for (int k = 0; k < N; k++)
-      if (k < left) v[k] += p.bias[j + k];
+    for (int k = 0; k < N; k++) v[k] += b[k];
   }
-  if (p.pre != nullptr) Piece<E>::store(static_cast<E*>(p.pre) + at, 0, left, v);
+  if (p.pre != nullptr) Piece<E>::store(static_cast<E*>(p.pre) + row, (int)j, (int)p.J, v);
   if (p.act != kActNone) {
 #pragma unroll
     for (int k = 0; k < N; k++) v[k] = act_of(v[k], p.act);
   }
   if (p.residual != nullptr) {
     float r[N];
-    Piece<E>::load(static_cast<const E*>(p.residual) + at, 0, left, r);
+    Piece<E>::load(static_cast<const E*>(p.residual) + row, (int)j, (int)p.J, r);
 #pragma unroll
     for (int k = 0; k < N; k++) v[k] += r[k];
   }
-  Piece<E>::store(static_cast<E*>(p.out) + at, 0, left, v);
+  Piece<E>::store(static_cast<E*>(p.out) + row, (int)j, (int)p.J, v);
 }
 
 }  // namespace la2

@@ -36,20 +36,6 @@ __device__ __forceinline__ f32x4 multiply16<float>(Piece<float>::vec a, Piece<fl
   return c;
 }
 
-// 16 bytes of a row of `width` elements, 0 behind its end (and for width 0)
-template <typename E>
-__device__ __forceinline__ typename Piece<E>::vec raw(const E* row, int64_t at, int64_t width) {
-  constexpr int N = Piece<E>::N;
-  typename Piece<E>::vec v;
-  if (at + N <= width) {
-    v = *reinterpret_cast<const typename Piece<E>::at_element*>(row + at);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = at + i < width ? row[at + i] : (E)0.f;
-  }
-  return v;
-}
-
 // A workgroup forms 16 outputs of IT * 16 rows: its waves share the reduction (a wave's lanes read 4 * 64 bytes of each of 16 rows of w at
 // a time), and meet in LDS.  x comes from the caches.
 template <typename E, int IT>
@@ -66,13 +52,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(ProductParam
   for (int64_t k = (int64_t)w * (4 * U * N); k < p.R; k += kFewWaves * 4 * U * N) {
     typename Piece<E>::vec fw[U], fx[IT][U];
 #pragma unroll
-    for (int u = 0; u < U; u++) fw[u] = raw(wrow, k + (4 * u + g) * N, wwidth);
+    for (int u = 0; u < U; u++) fw[u] = Piece<E>::raw(wrow, k + (4 * u + g) * N, wwidth);
 #pragma unroll
     for (int t = 0; t < IT; t++) {
       const int64_t i = 16 * t + l16;
       const E* xrow = static_cast<const E*>(p.a) + min(i, p.I - 1) * p.lda;
 #pragma unroll
-      for (int u = 0; u < U; u++) fx[t][u] = raw(xrow, k + (4 * u + g) * N, i < p.I ? p.R : 0);
+      for (int u = 0; u < U; u++) fx[t][u] = Piece<E>::raw(xrow, k + (4 * u + g) * N, i < p.I ? p.R : 0);
     }
 #pragma unroll
     for (int t = 0; t < IT; t++)
@@ -125,7 +111,7 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const E* from, int64_t 
   const int64_t pieces = ldo / N, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= rows * pieces) return;
   const int64_t row = at / pieces, col = at % pieces * N;
-  *reinterpret_cast<typename Piece<E>::vec*>(to + row * ldo + col) = raw(from + row * ld, col, width);
+  *reinterpret_cast<typename Piece<E>::vec*>(to + row * ldo + col) = Piece<E>::raw(from + row * ld, col, width);
 }
 
 // ---- dz and the bias' gradient
