@@ -6,22 +6,22 @@
 // tokens and its part of the softmax's sum; a second launch, one workgroup per batch row, joins the sums, scores those candidates
 // in 64 bits (so that a rounding makes no two of them equal) and takes the best.
 //
-// Both launches find the n largest the same way.  A wave's n-th largest of its lanes' maxima is found bit by bit, with the lanes' votes
-// (32 steps, no LDS); the largest of the waves' is a bound that at least n values reach.  The values that reach it (n or a few more;
-// at most n lanes of a wave hold any) go to LDS, where each one's rank is the number of larger ones.  Order and result do not depend
-// on the order in which threads arrive.
+// The n largest of a piece: the lanes form n groups or a few more; the smallest of the groups' maxima is a bound that at least n values
+// reach, and among values in no particular order n (1 + 1/2 + ... + 1/n) or so.  Those go to LDS, where each one's rank is the number of
+// larger ones.  Where more reach it than the list holds (many equal values) the n largest are taken one after the other.  The
+// candidates of the second launch are lists in order, which makes such a bound a poor one: there a wave's n-th largest of its lanes'
+// maxima is found bit by bit, with the lanes' votes, and the largest of the waves' is the bound (at most n lanes of a wave hold
+// anything that reaches it).  Order and result do not depend on the order in which threads arrive.
 #include "la2_layer.h"
 
 namespace la2 {
 namespace {
 
-constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectThreads = 256;
+constexpr int kList = 512;   // values that are ranked at once
 
-// A logit as what it counts for: NaN is no candidate, +inf is the largest finite value, the two zeros are one value.
-__device__ __forceinline__ float clean_logit(float x) {
-  if (x != x) return -INFINITY;
-  return fminf(x, 3.40282346638528859812e38f) + 0.f;
-}
+// A logit as what it counts for: NaN is no candidate, +inf is the largest finite value.
+__device__ __forceinline__ float clean_logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.40282346638528859812e38f); }
 
 // Unsigned numbers in the order of the floating ones, larger than 0 for all but -NaN, and back.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -36,22 +36,22 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 __device__ __forceinline__ double from_ordered(uint64_t u) {
   return __longlong_as_double((long long)(u >> 63 ? u & ~((uint64_t)1 << 63) : ~u));
 }
-// Larger logits first, then lower tokens; 0: no candidate.
+// Larger logits first (the two zeros are one), then lower tokens; 0: no candidate.
 __device__ __forceinline__ uint64_t key_of(float x, int token) {
-  return x == -INFINITY ? 0 : (uint64_t)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)token);
+  return x == -INFINITY ? 0 : (uint64_t)ordered(x + 0.f) << 32 | (0xFFFFFFFFu - (uint32_t)token);
 }
 
 __device__ __forceinline__ int votes(bool yes) { return __popcll(__ballot(yes)); }
 
-// The largest T that at least n of the `in` lanes' words reach (0 if there are fewer than n), and how many lanes are above it.
-__device__ __forceinline__ uint32_t nth_word(uint32_t word, bool in, int n, int& above) {
+// The largest T that at least n of the `in` lanes' words reach (0 if there are fewer than n), or a smaller one that exactly n reach.
+__device__ __forceinline__ uint32_t nth_word(uint32_t word, bool in, int n) {
   uint32_t t = 0;
-#pragma unroll 4
   for (int bit = 31; bit >= 0; bit--) {
     const uint32_t c = t | 1u << bit;
-    if (votes(in && word >= c) >= n) t = c;
+    const int reach = votes(in && word >= c);
+    if (reach >= n) t = c;
+    if (reach == n) break;
   }
-  above = votes(in && word > t);
   return t;
 }
 // A bound that exactly n of the wave's lanes reach, compared word by word (WORDS of them, the highest first); all words 0 if fewer than n
@@ -64,75 +64,82 @@ __device__ __forceinline__ void wave_bound(const uint32_t (&word)[WORDS], int n,
   if (votes(in) < n) return;
 #pragma unroll
   for (int k = 0; k < WORDS; k++) {
-    int above;
-    bound[k] = nth_word(word[k], in, n, above);
-    n -= above;
+    bound[k] = nth_word(word[k], in, n);
+    if (votes(in && word[k] >= bound[k]) == n) return;   // everything from here on
+    n -= votes(in && word[k] > bound[k]);
     in = in && word[k] == bound[k];
-    if (votes(in) == n) return;   // everything from here on
   }
 }
 
-// Workgroup (chunk, row): the largest of `parts` times P * 256 pieces of the row's vocabulary.
+// Workgroup (row, chunk): the largest of `parts` times P * 256 pieces of the row's vocabulary.
 template <typename T, int P>
 __global__ __launch_bounds__(kSelectThreads) void beam_chunk_kernel(BeamSelectParams p) {
-  constexpr int N = Piece<T>::N, PART = kSelectThreads * P * N;
-  __shared__ uint64_t found[kMaxBeams * kSelectWaves * P * N + kMaxBeams];   // at most n lanes a wave, and those of the parts before
-  __shared__ uint64_t best_of[kMaxBeams];
-  __shared__ float red[2][kSelectWaves];
-  __shared__ uint64_t bounds[kSelectWaves];
+  constexpr int N = Piece<T>::N, PART = kSelectThreads * P * N, WAVES = kSelectThreads / 64;
+  __shared__ uint64_t found[kList + kMaxBeams];
+  __shared__ uint64_t best_of[kMaxBeams];   // of the parts so far, in their order
+  __shared__ uint64_t round_best[2][WAVES];
+  __shared__ float high[WAVES][32], part_sum[WAVES];
   __shared__ int count;
-  const int row = blockIdx.x / p.chunks, n = p.beams, tid = threadIdx.x;
+  const int row = blockIdx.x / p.chunks, n = p.beams, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   if ((p.finished != nullptr && p.finished[row] != 0) || !(p.scores[row] > -INFINITY)) return;   // nothing of it is read
+  const int groups = n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : 32;   // lanes of one number modulo this
   const T* x = static_cast<const T*>(p.logits) + (int64_t)row * p.stride;
   const int begin = blockIdx.x % p.chunks * (p.parts * PART);
   const int end = min(p.vocab, begin + p.parts * PART);
   float largest = -INFINITY, total = 0.f;   // of the parts so far
   int kept = 0;
   for (int first = begin; first < end; first += PART) {
-    float v[P][N], m = -INFINITY;
-    int at = 0;
+    float v[P][N], m = -INFINITY, second = -INFINITY;   // a thread's largest two
 #pragma unroll
     for (int c = 0; c < P; c++) Piece<T>::load(x, first + (c * kSelectThreads + tid) * N, p.vocab, v[c]);
+    if (tid == 0) count = 0;
 #pragma unroll
-    for (int c = 0; c < P; c++)
+    for (int c = 0; c < P; c++) {
+      const int at = first + (c * kSelectThreads + tid) * N;
+      if (at + N <= p.vocab) {
+#pragma unroll
+        for (int i = 0; i < N; i++) v[c][i] = clean_logit(v[c][i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) v[c][i] = at + i < p.vocab ? clean_logit(v[c][i]) : -INFINITY;
+      }
 #pragma unroll
       for (int i = 0; i < N; i++) {
-        const int token = first + (c * kSelectThreads + tid) * N + i;
-        v[c][i] = token < p.vocab ? clean_logit(v[c][i]) : -INFINITY;
-        if (v[c][i] > m) {
-          m = v[c][i];
-          at = token;
-        }
+        second = __builtin_amdgcn_fmed3f(m, second, v[c][i]);
+        m = fmaxf(m, v[c][i]);
       }
-    const uint64_t best = key_of(m, at);
+    }
     float all = m;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) all = fmaxf(all, __shfl_xor(all, k));
-    const uint32_t words[2] = {(uint32_t)(best >> 32), (uint32_t)best};
-    uint32_t low[2];
-    wave_bound(words, n, low);
-    if ((tid & 63) == 0) {
-      red[0][tid >> 6] = all;
-      bounds[tid >> 6] = (uint64_t)low[0] << 32 | low[1];
-    }
-    if (tid == 0) count = 0;
+    for (int k = 32; k >= groups; k >>= 1) all = fmaxf(all, __shfl_xor(all, k));
+    if (lane < groups) high[wave][lane] = all;
     __syncthreads();
-    all = red[0][0];
-    uint64_t bound = bounds[0];
+    all = high[0][lane % groups];
 #pragma unroll
-    for (int w = 1; w < kSelectWaves; w++) {
-      all = fmaxf(all, red[0][w]);
-      bound = bounds[w] > bound ? bounds[w] : bound;
+    for (int w = 1; w < WAVES; w++) all = fmaxf(all, high[w][lane % groups]);
+    float bound = all;
+    for (int k = 1; k < groups; k <<= 1) {
+      all = fmaxf(all, __shfl_xor(all, k));
+      bound = fminf(bound, __shfl_xor(bound, k));
     }
-    if (kept == n) bound = best_of[n - 1] > bound ? best_of[n - 1] : bound;   // (kept in the order of rank)
-    if (best != 0 && best >= bound) {
+    if (kept == n) bound = fmaxf(bound, from_ordered((uint32_t)(best_of[n - 1] >> 32)));
+    if (m > -INFINITY && m >= bound) {
+      int at = 0;   // the first of the thread's largest
 #pragma unroll
-      for (int c = 0; c < P; c++)
+      for (int c = P - 1; c >= 0; c--)
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-          const uint64_t key = key_of(v[c][i], first + (c * kSelectThreads + tid) * N + i);
-          if (key != 0 && key >= bound) found[atomicAdd(&count, 1)] = key;
-        }
+        for (int i = N - 1; i >= 0; i--) at = v[c][i] == m ? c * N + i : at;
+      const int to = atomicAdd(&count, 1);
+      if (to < kList) found[to] = key_of(m, first + (at / N * kSelectThreads + tid) * N + at % N);
+      if (second > -INFINITY && second >= bound) {
+#pragma unroll
+        for (int c = 0; c < P; c++)
+#pragma unroll
+          for (int i = 0; i < N; i++)
+            if (v[c][i] > -INFINITY && v[c][i] >= bound && c * N + i != at) {
+              const int to = atomicAdd(&count, 1);
+              if (to < kList) found[to] = key_of(v[c][i], first + (c * kSelectThreads + tid) * N + i);
+            }
+      }
     }
     float sum = 0.f;
     if (all > -INFINITY) {
@@ -143,28 +150,55 @@ __global__ __launch_bounds__(kSelectThreads) void beam_chunk_kernel(BeamSelectPa
 #pragma unroll
       for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
     }
-    if ((tid & 63) == 0) red[1][tid >> 6] = sum;
+    if (lane == 0) part_sum[wave] = sum;
     __syncthreads();
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; w++) sum += red[1][w];
     if (all > -INFINITY) {
+      sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) sum += part_sum[w];
       const float top = fmaxf(all, largest);
       total = total * (largest > -INFINITY ? __expf(largest - top) : 0.f) + sum * __expf(all - top);
       largest = top;
     }
     const int fresh = count;
-    if (tid < kept) found[fresh + tid] = best_of[tid];
-    __syncthreads();
-    const int have = fresh + kept;
-    for (int c = tid; c < have; c += kSelectThreads) {
-      const uint64_t key = found[c];
-      int larger = 0;
+    if (fresh <= kList) {
+      if (tid < kept) found[fresh + tid] = best_of[tid];
+      __syncthreads();
+      const int have = fresh + kept;
+      for (int c = tid; c < have; c += kSelectThreads) {
+        const uint64_t key = found[c];
+        int larger = 0;
 #pragma unroll 4
-      for (int k = 0; k < have; k++) larger += found[k] > key;
-      if (larger < n) best_of[larger] = key;
+        for (int k = 0; k < have; k++) larger += found[k] > key;
+        if (larger < n) best_of[larger] = key;
+      }
+      kept = min(n, have);
+    } else {   // one after the other
+      const uint64_t before = tid < kept ? best_of[tid] : 0;
+      uint64_t last = ~(uint64_t)0;
+      for (kept = 0; kept < n; kept++) {
+        uint64_t best = before < last ? before : 0;
+#pragma unroll
+        for (int c = 0; c < P; c++)
+#pragma unroll
+          for (int i = 0; i < N; i++) {
+            const uint64_t key = key_of(v[c][i], first + (c * kSelectThreads + tid) * N + i);
+            best = key < last && key > best ? key : best;
+          }
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) {
+          const uint64_t other = __shfl_xor((unsigned long long)best, k);
+          best = other > best ? other : best;
+        }
+        if (lane == 0) round_best[kept & 1][wave] = best;
+        __syncthreads();
+        last = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) last = round_best[kept & 1][w] > last ? round_best[kept & 1][w] : last;
+        if (last == 0) break;   // (more than kList values: there are n)
+        if (tid == 0) best_of[kept] = last;
+      }
     }
-    kept = min(n, have);
     __syncthreads();
   }
   const int64_t to = (int64_t)blockIdx.x;   // row * chunks + chunk

@@ -85,6 +85,21 @@ __device__ __forceinline__ void load_floats(const float* p, int64_t at, int64_t 
   }
 }
 
+// ... and their way back; the vector may start at any float
+template <int N>
+__device__ __forceinline__ void store_floats(float* p, int64_t at, int64_t width, const float (&v)[N]) {
+  typedef __attribute__((ext_vector_type(4))) float f4;
+  typedef f4 at_float __attribute__((aligned(4)));
+  if (at + N <= width) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<at_float*>(p + at + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++)
+      if (at + i < width) p[at + i] = v[i];
+  }
+}
+
 struct LayerNormParams {
   int64_t rows;
   int32_t width;
@@ -101,6 +116,8 @@ struct LayerNormParams {
   float* d_bias;
   float* partial;        // [workgroups][2][width]
 };
+// a[j] and, from j = first on, b[j - first] = the sums of columns j over `count` rows of partial, in a fixed order
+hipError_t launch_column_sums(const float* partial, int64_t count, int64_t columns, int64_t first, float* a, float* b, hipStream_t s);
 hipError_t launch_layer_norm_fwd(int dtype, const LayerNormParams& p, int units, hipStream_t s);
 hipError_t launch_layer_norm_bwd(int dtype, const LayerNormParams& p, int units, hipStream_t s);
 // rows of partial sums that the backward pass writes; 0: it needs none

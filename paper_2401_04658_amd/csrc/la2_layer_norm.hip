@@ -101,8 +101,9 @@ template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(LayerNormParams p) {
   constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
-  __shared__ float2 share[RPB > 1 ? TPR * CH * N : 1];
+  __shared__ __align__(16) float share[RPB > 1 ? 2 * RPB * TPR * CH * N : 4];   // dw, then db: the rows' groups' sums, in the order of columns
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  constexpr bool AHEAD = CH * N <= 16 && TPR < 1024;   // (registers)
   constexpr bool KEEP = CH * N <= 16;   // the weights stay in registers; else they come from the caches, twice a row
   float w[CH][N], aw[CH][N], ab[CH][N];
 #pragma unroll
@@ -113,17 +114,35 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   }
   const float width = (float)p.width;
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
+  // The row as it is stored (h and g are formed twice rather than kept), and the next one, on its way meanwhile
+  typename Piece<T>::vec rx[CH], rg[CH], nx[CH], ng[CH];
+  float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  auto fetch = [&](int64_t row) {
+    if (row >= p.rows) return;
+    const int end = renewed(p.width);
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
     const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
-    const float mean = p.mean[row], rstd = p.rstd[row];
-    const int end = renewed(p.width);
-    typename Piece<T>::vec rx[CH], rg[CH];   // the row as it is stored: h and g are formed twice rather than kept
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      rx[c] = Piece<T>::raw(x, (c * TPR + lane) * N, end);
-      rg[c] = Piece<T>::raw(dy, (c * TPR + lane) * N, end);
+      nx[c] = Piece<T>::raw(x, (c * TPR + lane) * N, end);
+      ng[c] = Piece<T>::raw(dy, (c * TPR + lane) * N, end);
     }
+    next_mean = p.mean[row];
+    next_rstd = p.rstd[row];
+  };
+  int64_t row = (int64_t)blockIdx.x * RPB + sub;
+  fetch(row);
+  for (; row < p.rows; row += step, turn ^= 1) {
+    const int end = renewed(p.width);
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      rx[c] = nx[c];
+      rg[c] = ng[c];
+    }
+    mean = next_mean;
+    rstd = next_rstd;
+    if (AHEAD) fetch(row + step);
     float sg = 0.f, sh = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
@@ -152,39 +171,41 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
       for (int i = 0; i < N; i++) v[i] = rstd * ((float)rg[c][i] * w[c][i] - mg - ((float)rx[c][i] - mean) * rstd * mh);
       Piece<T>::store(dx, (c * TPR + lane) * N, end, v);
     }
+    if (!AHEAD) fetch(row + step);
   }
   if (p.d_weight == nullptr && p.d_bias == nullptr) return;
-  if constexpr (RPB > 1) {
-    for (int r = 0; r < RPB; r++) {
-      if (sub == r) {
-#pragma unroll
-        for (int c = 0; c < CH; c++)
-#pragma unroll
-          for (int i = 0; i < N; i++) {
-            float2& at = share[(c * N + i) * TPR + lane];
-            if (r > 0) {
-              aw[c][i] += at.x;
-              ab[c][i] += at.y;
-            }
-            if (r < RPB - 1) at = make_float2(aw[c][i], ab[c][i]);
-          }
-      }
-      __syncthreads();
-    }
-    if (sub != RPB - 1) return;
-  }
   const bool only = gridDim.x == 1;
   float* ow = only ? p.d_weight : p.partial + (int64_t)blockIdx.x * 2 * p.width;
   float* ob = only ? p.d_bias : p.partial + ((int64_t)blockIdx.x * 2 + 1) * p.width;
+  if constexpr (RPB > 1) {
+    constexpr int COLS = TPR * CH * N;
 #pragma unroll
-  for (int c = 0; c < CH; c++)
+    for (int c = 0; c < CH; c++)
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      const int j = (c * TPR + lane) * N + i;
-      if (j >= p.width) continue;
-      if (ow != nullptr) ow[j] = aw[c][i];
-      if (ob != nullptr) ob[j] = ab[c][i];
+      for (int i = 0; i < N; i += 4) {
+        const int at = sub * COLS + (c * TPR + lane) * N + i;
+        *reinterpret_cast<float4*>(share + at) = make_float4(aw[c][i], aw[c][i + 1], aw[c][i + 2], aw[c][i + 3]);
+        *reinterpret_cast<float4*>(share + RPB * COLS + at) = make_float4(ab[c][i], ab[c][i + 1], ab[c][i + 2], ab[c][i + 3]);
+      }
+    __syncthreads();
+    for (int j = threadIdx.x; j < min(COLS, p.width); j += Shape<TPR>::kThreads) {
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int r = 0; r < RPB; r++) {
+        a += share[r * COLS + j];
+        b += share[(RPB + r) * COLS + j];
+      }
+      if (ow != nullptr) ow[j] = a;
+      if (ob != nullptr) ob[j] = b;
     }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const int at = (c * TPR + lane) * N;
+      if (ow != nullptr) store_floats(ow, at, p.width, aw[c]);
+      if (ob != nullptr) store_floats(ob, at, p.width, ab[c]);
+    }
+  }
 }
 
 // Rows that no group of lanes holds in registers: they are read again for every pass over them, from the caches.
@@ -249,30 +270,6 @@ __global__ __launch_bounds__(256) void layer_norm_wide_columns_kernel(LayerNormP
   p.partial[((int64_t)blockIdx.y * 2 + 1) * p.width + j] = ab;
 }
 
-// d_weight, d_bias = the sums over `count` rows of partial: 16 columns a workgroup, 16 threads each
-__global__ __launch_bounds__(256) void layer_norm_sum_kernel(const float* partial, int64_t count, int32_t width, float* d_weight,
-                                                             float* d_bias) {
-  __shared__ float part[16][16 + 1];
-  const int col = threadIdx.x % 16, slice = threadIdx.x / 16;
-  const int64_t j = (int64_t)blockIdx.x * 16 + col, all = 2 * (int64_t)width;
-  float a = 0.f;
-  if (j < all) {
-#pragma unroll 8
-    for (int64_t r = slice; r < count; r += 16) a += partial[r * all + j];
-  }
-  part[slice][col] = a;
-  __syncthreads();
-  if (slice != 0 || j >= all) return;
-  a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; i++) a += part[i][col];
-  if (j < width) {
-    if (d_weight != nullptr) d_weight[j] = a;
-  } else if (d_bias != nullptr) {
-    d_bias[j - width] = a;
-  }
-}
-
 template <int TPR, int CH>
 struct Split {
   static constexpr int tpr = TPR, ch = CH;
@@ -286,14 +283,17 @@ auto split_of(int32_t width, F f) {
   if (pieces <= 32) return f(Split<32, 1>{});
   if (pieces <= 64) return f(Split<64, 1>{});
   if (pieces <= 128) return f(Split<64, 2>{});
-  if constexpr (!BWD)
+  if constexpr (!BWD || sizeof(T) == 4)
     if (pieces <= 256) return f(Split<64, 4>{});
-  if (pieces <= 256) return f(Split<256, 1>{});
+  if constexpr (BWD && sizeof(T) == 2)
+    if (pieces <= 256) return f(Split<256, 1>{});
   if (pieces <= 512) return f(Split<256, 2>{});
   if (pieces <= 1024) return f(Split<512, 2>{});
-  if constexpr (BWD && sizeof(T) == 2)   // 32 elements a lane do not fit the registers beside their sums
+  if constexpr (BWD && sizeof(T) == 2) {   // 32 elements a lane do not fit the registers beside their sums
     if (pieces <= 2048) return f(Split<1024, 2>{});
-  if (pieces <= 2048) return f(Split<512, 4>{});
+  } else {
+    if (pieces <= 2048) return f(Split<512, 4>{});
+  }
   return f(Split<0, 0>{});
 }
 
@@ -304,7 +304,7 @@ int64_t groups(int64_t rows, int units, int most) {
   const int64_t fit = (int64_t)units * (TPR > 256 ? 2 : most);
   return need < 1 ? 1 : need < fit ? need : fit;   // no rows: one, which sets the gradients to 0
 }
-constexpr int kFwdPerUnit = 8, kBwdPerUnit = 4;
+constexpr int kFwdPerUnit = 8, kBwdPerUnit = 2;
 
 template <typename T>
 hipError_t fwd(const LayerNormParams& p, int units, hipStream_t s) {
@@ -346,12 +346,40 @@ hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || !sums || count == 0) return e;
-  hipLaunchKernelGGL(layer_norm_sum_kernel, dim3((unsigned)((2 * (int64_t)p.width + 15) / 16)), dim3(256), 0, s, p.partial, count, p.width,
-                     p.d_weight, p.d_bias);
-  return hipGetLastError();
+  return launch_column_sums(p.partial, count, 2 * (int64_t)p.width, p.width, p.d_weight, p.d_bias, s);
 }
 
 }  // namespace
+
+// 16 columns a workgroup, 64 threads each
+constexpr int kSumCols = 16, kSumSlices = 64;
+__global__ __launch_bounds__(kSumCols * kSumSlices) void column_sum_kernel(const float* partial, int64_t count, int64_t columns, int64_t first,
+                                                                           float* a, float* b) {
+  __shared__ float part[kSumSlices][kSumCols + 1];
+  const int col = threadIdx.x % kSumCols, slice = threadIdx.x / kSumCols;
+  const int64_t j = (int64_t)blockIdx.x * kSumCols + col;
+  float v = 0.f;
+  if (j < columns) {
+#pragma unroll 8
+    for (int64_t r = slice; r < count; r += kSumSlices) v += partial[r * columns + j];
+  }
+  part[slice][col] = v;
+  __syncthreads();
+  if (slice != 0 || j >= columns) return;
+  v = 0.f;
+#pragma unroll 16
+  for (int i = 0; i < kSumSlices; i++) v += part[i][col];
+  if (j < first) {
+    if (a != nullptr) a[j] = v;
+  } else if (b != nullptr) {
+    b[j - first] = v;
+  }
+}
+hipError_t launch_column_sums(const float* partial, int64_t count, int64_t columns, int64_t first, float* a, float* b, hipStream_t s) {
+  hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((columns + kSumCols - 1) / kSumCols)), dim3(kSumCols * kSumSlices), 0, s, partial, count,
+                     columns, first, a, b);
+  return hipGetLastError();
+}
 
 hipError_t launch_layer_norm_fwd(int dtype, const LayerNormParams& p, int units, hipStream_t s) {
   if (dtype == kBF16) return fwd<__bf16>(p, units, s);

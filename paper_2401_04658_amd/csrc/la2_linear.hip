@@ -162,23 +162,6 @@ __global__ __launch_bounds__(kSlopeCols * kSlopeRows) void linear_slope_kernel(S
   }
 }
 
-__global__ __launch_bounds__(256) void linear_sum_kernel(const float* partial, int32_t count, int32_t width, float* out) {
-  __shared__ float part[16][16 + 1];
-  const int col = threadIdx.x % 16, slice = threadIdx.x / 16, j = blockIdx.x * 16 + col;
-  float a = 0.f;
-  if (j < width) {
-#pragma unroll 8
-    for (int r = slice; r < count; r += 16) a += partial[(int64_t)r * width + j];
-  }
-  part[slice][col] = a;
-  __syncthreads();
-  if (slice != 0 || j >= width) return;
-  a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; i++) a += part[i][col];
-  out[j] = a;
-}
-
 // ---- host side
 size_t elem(int dtype) { return dtype == kF32 ? 4 : 2; }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -338,9 +321,8 @@ hipError_t backward(const LinearParams& q, Taker& t, bool count_only, int units,
       if (d == kBF16) slope<__bf16>(sp, grid, s);
       else if (d == kF16) slope<_Float16>(sp, grid, s);
       else slope<float>(sp, grid, s);
-      if (q.d_bias != nullptr)
-        hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)((q.out + 15) / 16)), dim3(256), 0, s, sp.partial, (int32_t)blocks, q.out, q.d_bias);
-      const hipError_t e = hipGetLastError();
+      hipError_t e = hipGetLastError();
+      if (e == hipSuccess && q.d_bias != nullptr) e = launch_column_sums(sp.partial, blocks, q.out, q.out, q.d_bias, nullptr, s);
       if (e != hipSuccess) return e;
     }
   }
