@@ -85,6 +85,17 @@ __device__ __forceinline__ void load_floats(const float* p, int64_t at, int64_t 
   }
 }
 
+// The same from any float on, 0 behind the end
+template <int N>
+__device__ __forceinline__ void load_any_floats(const float* p, int64_t at, int64_t width, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const auto u = Piece<float>::raw(p, at + i, width);
+#pragma unroll
+    for (int k = 0; k < 4; k++) v[i + k] = u[k];
+  }
+}
+
 // ... and their way back; the vector may start at any float
 template <int N>
 __device__ __forceinline__ void store_floats(float* p, int64_t at, int64_t width, const float (&v)[N]) {

@@ -52,75 +52,88 @@ size_t linear_bwd_workspace(const LinearParams& p, int units);
 hipError_t launch_linear_fwd(const LinearParams& p, void* workspace, int units, hipStream_t s);
 hipError_t launch_linear_bwd(const LinearParams& p, void* workspace, int units, hipStream_t s);
 
-enum { kTile64 = 0, kTile128 = 1, kTile256 = 2 };
-hipError_t launch_product_bf16(int tile, bool across_a, bool across_b, const ProductParams& p, hipStream_t s);
-hipError_t launch_product_f16(int tile, bool across_a, bool across_b, const ProductParams& p, hipStream_t s);
-hipError_t launch_product_f32(int tile, bool across_a, bool across_b, const ProductParams& p, hipStream_t s);
+// Both products of a backward pass (the input's gradient: a along, b across; the weight's: both across) in one launch, workgroups
+// [0, first) the one with the longer way, and behind them those that sum the columns of `partial` into d_bias.
+struct PairParams {
+  ProductParams p[2];        // 0: the input's gradient, 1: the weight's
+  int32_t groups[2];         // workgroups of each; 0: not wanted
+  int32_t weight_first;
+  const float* partial;      // [count][width], nullptr: no sums
+  int32_t count, width;
+  float* sums;
+};
 
-// erfc(z) for z >= 0 as exp(-z^2) times a polynomial in 1 / (1 + 0.3275911 z): Abramowitz and Stegun, Handbook of Mathematical
-// Functions, 7.1.26 (absolute error 1.5e-7).  `e` = exp(-z^2).
-__device__ __forceinline__ float erfc_from(float z, float e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
-  float s = fmaf(1.061405429f, t, -1.453152027f);
-  s = fmaf(s, t, 1.421413741f);
-  s = fmaf(s, t, -0.284496736f);
-  s = fmaf(s, t, 0.254829592f);
-  return s * t * e;
-}
+enum { kTile64 = 0, kTile128 = 1, kTile256 = 2, kTiles = 3 };
+hipError_t launch_product_bf16(int tile, const ProductParams& p, hipStream_t s);
+hipError_t launch_product_f16(int tile, const ProductParams& p, hipStream_t s);
+hipError_t launch_product_f32(int tile, const ProductParams& p, hipStream_t s);
+hipError_t launch_pair_bf16(int tile, const PairParams& p, hipStream_t s);
+hipError_t launch_pair_f16(int tile, const PairParams& p, hipStream_t s);
+hipError_t launch_pair_f32(int tile, const PairParams& p, hipStream_t s);
+
+// exp(-x^2 / 2) and the normal distribution's tail Phi(-a) at a = min(|x|, 64), as exp(-z^2) times a polynomial in 1 / (1 + 0.3275911 z), z = a /
+// sqrt(2): Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7 of erfc, half of that here).
 constexpr float kHalfRoot = 0.70710678118654752440f, kLog2e = 1.44269504088896340736f;
-// The normal distribution function at x, and exp(-x^2 / 2)
-__device__ __forceinline__ float normal_cdf(float x, float& e) {
-  const float z = fabsf(x) * kHalfRoot;
-  e = __builtin_amdgcn_exp2f(-z * z * kLog2e);
-  const float tail = 0.5f * erfc_from(z, e);
-  return x < 0.f ? tail : 1.f - tail;
+__device__ __forceinline__ float normal_tail(float x, float& a, float& e) {
+  a = fminf(fabsf(x), 64.f);
+  e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * kHalfRoot, a, 1.f));
+  float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  s = fmaf(s, t, 0.5f * 1.421413741f);
+  s = fmaf(s, t, 0.5f * -0.284496736f);
+  s = fmaf(s, t, 0.5f * 0.254829592f);
+  return s * t * e;
 }
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2e)); }
 
-// act(z) and its slope.  An infinite z keeps the limits: 0 * inf is not formed.
-__device__ __forceinline__ float act_of(float z, int act) {
-  if (act == kActRelu) return z > 0.f ? z : z == z ? 0.f : z;
-  if (act == kActGelu) {
-    float e;
-    const float c = normal_cdf(z, e);
-    return c == 0.f ? 0.f : z * c;
+// act(z) and its slope.  Factors that may be infinite are cut where the other factor has become 0; a NaN comes through the other factor.
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+  if (ACT == kActRelu) return z > 0.f ? z : z == z ? 0.f : z;
+  if (ACT == kActGelu) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+    float a, e;
+    const float tail = normal_tail(z, a, e);
+    return fmaf(-a, tail, fmaxf(z, 0.f));
   }
-  if (act == kActSilu) {
-    const float c = sigmoid(z);
-    return c == 0.f ? 0.f : z * c;
-  }
+  if (ACT == kActSilu) return fmaxf(z, -2000.f) * sigmoid(z);
   return z;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
-  if (act == kActRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
-  if (act == kActGelu) {
-    float e;
-    const float c = normal_cdf(z, e);
-    return e == 0.f ? c : fmaf(z * 0.39894228040143267794f, e, c);   // 1 / sqrt(2 pi)
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if (ACT == kActRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
+  if (ACT == kActGelu) {   // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
+    float a, e;
+    const float tail = normal_tail(z, a, e);
+    return fmaf(copysignf(a, z) * 0.39894228040143267794f, e, z < 0.f ? tail : 1.f - tail);
   }
-  if (act == kActSilu) {
+  if (ACT == kActSilu) {
     const float c = sigmoid(z);
-    return c == 0.f ? 0.f : c == 1.f ? 1.f : c * fmaf(z, 1.f - c, 1.f);
+    return c * fmaf(fminf(fmaxf(z, -2000.f), 2000.f), 1.f - c, 1.f);
   }
   return 1.f;
 }
+template <int ACT>
+struct Act {
+  static constexpr int value = ACT;
+};
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  if (act == kActNone) f(Act<kActNone>{});
+  else if (act == kActRelu) f(Act<kActRelu>{});
+  else if (act == kActGelu) f(Act<kActGelu>{});
+  else f(Act<kActSilu>{});
+}
 
-// N sums of row i from column j on, finished: bias, pre, activation, residual, rounded once.
-template <typename E, int N>
-__device__ __forceinline__ void finish(const ProductParams& p, int64_t i, int64_t j, float (&v)[N]) {
+// N sums of row i from column j on, finished: bias (b), pre, activation, residual, rounded once.
+template <typename E, int ACT, int N>
+__device__ __forceinline__ void finish(const ProductParams& p, int64_t i, int64_t j, const float (&b)[N], float (&v)[N]) {
   static_assert(N == Piece<E>::N, "one piece");
   const int64_t row = i * p.ldo;
-  if (p.bias != nullptr) {
-    float b[N];
-    load_floats(p.bias, j, p.J, 0.f, b);
 #pragma unroll
-    for (int k = 0; k < N; k++) v[k] += b[k];
-  }
+  for (int k = 0; k < N; k++) v[k] += b[k];
   if (p.pre != nullptr) Piece<E>::store(static_cast<E*>(p.pre) + row, (int)j, (int)p.J, v);
-  if (p.act != kActNone) {
 #pragma unroll
-    for (int k = 0; k < N; k++) v[k] = act_of(v[k], p.act);
-  }
+  for (int k = 0; k < N; k++) v[k] = act_of<ACT>(v[k]);
   if (p.residual != nullptr) {
     float r[N];
     Piece<E>::load(static_cast<const E*>(p.residual) + row, (int)j, (int)p.J, r);

@@ -1,8 +1,7 @@
-// The tiled matrix product for f32 operands (la2_linear_tiles.h).
+// The tiled matrix products of f32 operands (la2_linear_tiles.h).
 #include "la2_linear_tiles.h"
 
 namespace la2 {
-hipError_t launch_product_f32(int tile, bool across_a, bool across_b, const ProductParams& p, hipStream_t s) {
-  return linear::launch_product<float>(tile, across_a, across_b, p, s);
-}
+hipError_t launch_product_f32(int tile, const ProductParams& p, hipStream_t s) { return linear::launch_product<float>(tile, p, s); }
+hipError_t launch_pair_f32(int tile, const PairParams& p, hipStream_t s) { return linear::launch_pair<float>(tile, p, s); }
 }  // namespace la2

@@ -168,22 +168,34 @@ __device__ __forceinline__ void place(uint32_t wg, uint32_t tiles_i, uint32_t ti
   tj = in / height;
 }
 
-template <typename E, int TI, int TJ, int WI, int WJ, bool AA, bool AB>
-__global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductParams p) {
-  constexpr int NW = WI * WJ, NI = TI / WI / 32, NJ = TJ / WJ / 32;
+template <int N>
+__device__ __forceinline__ void wait_loads() {   // until at most N of this wave's loads are on their way
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// A tile's shape: TI x TJ, WI x WJ waves, STAGES buffers
+template <int TI_, int TJ_, int WI_, int WJ_, int STAGES_>
+struct Shape {
+  static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, STAGES = STAGES_, NW = WI * WJ, THREADS = 64 * NW;
+  static constexpr int BYTES = (TI + TJ) * kStepBytes * STAGES;
+};
+
+// Workgroup `wg` of the tiles of p
+template <typename E, typename S, bool AA, bool AB>
+__device__ __forceinline__ void product(const ProductParams& p, uint32_t wg, char* lds) {
+  constexpr int TI = S::TI, TJ = S::TJ, WJ = S::WJ, NW = S::NW, NI = TI / S::WI / 32, NJ = TJ / WJ / 32, STAGES = S::STAGES;
   constexpr int KE = kStepBytes / (int)sizeof(E), GROUPS = kStepBytes / 32;
   using A = Operand<E, TI, AA, NW>;
   using B = Operand<E, TJ, AB, NW>;
-  constexpr int STAGE = A::BYTES + B::BYTES;
+  constexpr int STAGE = A::BYTES + B::BYTES, LOADS = A::LOADS + B::LOADS;
   constexpr int ROWF = 32 * NJ + 4;   // floats of a row in the epilogue's staging
-  static_assert(NW * 32 * ROWF * 4 <= 2 * STAGE, "the staging fits");
-  __shared__ __align__(1024) char lds[2 * STAGE];
+  static_assert(NW * 32 * ROWF * 4 <= S::BYTES && STAGE * STAGES == S::BYTES, "the staging fits");
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), wi = w / WJ, wj = w % WJ;
   uint32_t ti, tj;
   const uint32_t tiles_i = (uint32_t)((p.I + TI - 1) / TI), tiles_j = (uint32_t)((p.J + TJ - 1) / TJ);
-  const uint32_t split = blockIdx.x / (tiles_i * tiles_j);
-  place(blockIdx.x % (tiles_i * tiles_j), tiles_i, tiles_j, ti, tj);
+  const uint32_t split = wg / (tiles_i * tiles_j);
+  place(wg % (tiles_i * tiles_j), tiles_i, tiles_j, ti, tj);
   const int64_t i0 = (int64_t)ti * TI, j0 = (int64_t)tj * TJ, r0 = split * p.span, r1 = min(p.R, r0 + p.span);
 
   f32x16 acc[NI][NJ];
@@ -197,96 +209,154 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductParams p) 
   a.start(p.a, p.lda, i0, p.I, r0, r1, w, lane);
   b.start(p.b, p.ldb, j0, p.J, r0, r1, w, lane);
   const uint32_t at = lds_offset(lds);
-  int rem = (int)(r1 - r0);
+  int rem = (int)(r1 - r0);   // of the reduction, from the next step to be loaded on
   const int steps = (rem + KE - 1) / KE;
-  if (steps > 0) {
+  auto load = [&](int stage) {
 #pragma unroll
-    for (int k = 0; k < A::LOADS; k++) a.load(k, at, rem);
+    for (int k = 0; k < A::LOADS; k++) a.load(k, at + stage * STAGE, rem);
 #pragma unroll
-    for (int k = 0; k < B::LOADS; k++) b.load(k, at + A::BYTES, rem);
-  }
+    for (int k = 0; k < B::LOADS; k++) b.load(k, at + stage * STAGE + A::BYTES, rem);
+    a.advance();
+    b.advance();
+    rem -= KE;
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; s++)
+    if (s < steps) load(s);
+  int here = 0, next = STAGES - 1;
   for (int t = 0; t < steps; t++) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    lds_barrier();   // this step's tiles are there, and nobody reads the other buffer any more
-    const char* here = lds + (t & 1) * STAGE;
-    const uint32_t next = at + ((t + 1) & 1) * STAGE;
-    const bool more = t + 1 < steps;
-    if (more) {
-      a.advance();
-      b.advance();
-      rem -= KE;
-#pragma unroll
-      for (int k = 0; k < A::LOADS; k++) a.load(k, next, rem);
-#pragma unroll
-      for (int k = 0; k < B::LOADS; k++) b.load(k, next + A::BYTES, rem);
-    }
+    if (t + STAGES - 1 <= steps) wait_loads<(STAGES - 2) * LOADS>();   // this step's have arrived: those of STAGES - 2 behind it are under way
+    else wait_loads<0>();
+    lds_barrier();   // everybody's have, and nobody reads the buffer of the step before any more
+    if (t + STAGES - 1 < steps) load(next);
+    const char* tile = lds + here * STAGE;
 #pragma unroll
     for (int g = 0; g < GROUPS; g++) {
       Frag<E> fa[NI], fb[NJ];
 #pragma unroll
-      for (int i = 0; i < NI; i++) fa[i] = read<E, TI, AA>(here, wi * NI + i, g, lane);
+      for (int i = 0; i < NI; i++) fa[i] = read<E, TI, AA>(tile, wi * NI + i, g, lane);
 #pragma unroll
-      for (int j = 0; j < NJ; j++) fb[j] = read<E, TJ, AB>(here + A::BYTES, wj * NJ + j, g, lane);
+      for (int j = 0; j < NJ; j++) fb[j] = read<E, TJ, AB>(tile + A::BYTES, wj * NJ + j, g, lane);
 #pragma unroll
       for (int i = 0; i < NI; i++)
 #pragma unroll
         for (int j = 0; j < NJ; j++) acc[i][j] = multiply<E>(fb[j], fa[i], acc[i][j]);
     }
+    here = here + 1 == STAGES ? 0 : here + 1;
+    next = next + 1 == STAGES ? 0 : next + 1;
   }
   lds_barrier();   // the tiles are done with: each wave stages its rows in its own part of them
 
-  constexpr int N = Piece<E>::N, LPR = 32 * NJ / N;   // lanes of a row
+  constexpr int N = Piece<E>::N, LPR = 32 * NJ / N, RPI = 64 / LPR;   // lanes of a row, rows of an instruction
   float* stage = reinterpret_cast<float*>(lds) + w * 32 * ROWF;
   const int l32 = lane & 31, hh = lane >> 5;
+  const int row0 = lane / LPR, col = lane % LPR * N;
+  const int64_t cj = j0 + wj * NJ * 32 + col;
+  float bias[N];
+  load_floats(p.splits == 1 ? p.bias : nullptr, cj, p.J, 0.f, bias);
+  with_act(p.act, [&](auto act) {
 #pragma unroll
-  for (int i = 0; i < NI; i++) {
+    for (int i = 0; i < NI; i++) {
 #pragma unroll
-    for (int j = 0; j < NJ; j++)
+      for (int j = 0; j < NJ; j++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const bf16k::f32x4 four = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        *reinterpret_cast<bf16k::f32x4*>(stage + l32 * ROWF + 32 * j + 8 * q + 4 * hh) = four;
-      }
+        for (int q = 0; q < 4; q++) {
+          const bf16k::f32x4 four = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          *reinterpret_cast<bf16k::f32x4*>(stage + l32 * ROWF + 32 * j + 8 * q + 4 * hh) = four;
+        }
+      if (cj >= p.J) continue;
 #pragma unroll
-    for (int k = 0; k < 32 * LPR / 64; k++) {
-      const int row = (k * 64 + lane) / LPR, col = (k * 64 + lane) % LPR * N;
-      float v[N];
+      for (int k = 0; k < 32 / RPI; k++) {
+        const int row = k * RPI + row0;
+        const int64_t ci = i0 + (wi * NI + i) * 32 + row;
+        if (ci >= p.I) continue;
+        float v[N];
 #pragma unroll
-      for (int e = 0; e < N; e += 4) {
-        const bf16k::f32x4 four = *reinterpret_cast<const bf16k::f32x4*>(stage + row * ROWF + col + e);
+        for (int e = 0; e < N; e += 4) {
+          const bf16k::f32x4 four = *reinterpret_cast<const bf16k::f32x4*>(stage + row * ROWF + col + e);
 #pragma unroll
-        for (int f = 0; f < 4; f++) v[e + f] = four[f];
-      }
-      const int64_t ci = i0 + (wi * NI + i) * 32 + row, cj = j0 + wj * NJ * 32 + col;
-      if (ci >= p.I || cj >= p.J) continue;
-      if (p.splits == 1) {
-        finish<E, N>(p, ci, cj, v);
-      } else {
-        float* out = p.partial + (split * p.I + ci) * p.J + cj;
-        const int left = (int)min(p.J - cj, (int64_t)N);
-#pragma unroll
-        for (int e = 0; e < N; e++)
-          if (e < left) out[e] = v[e];
+          for (int f = 0; f < 4; f++) v[e + f] = four[f];
+        }
+        if (p.splits == 1) finish<E, decltype(act)::value, N>(p, ci, cj, bias, v);
+        else store_floats(p.partial + (split * p.I + ci) * p.J, cj, p.J, v);
       }
     }
-  }
+  });
 }
 
-template <typename E, int TI, int TJ, int WI, int WJ>
-hipError_t launch_tile(bool aa, bool ab, const ProductParams& p, hipStream_t s) {
-  const int64_t tiles = ((p.I + TI - 1) / TI) * ((p.J + TJ - 1) / TJ);
-  const dim3 grid((unsigned)(tiles * p.splits)), block(64 * WI * WJ);
-  if (!aa && !ab) hipLaunchKernelGGL((product_kernel<E, TI, TJ, WI, WJ, false, false>), grid, block, 0, s, p);
-  else if (!aa) hipLaunchKernelGGL((product_kernel<E, TI, TJ, WI, WJ, false, true>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((product_kernel<E, TI, TJ, WI, WJ, true, true>), grid, block, 0, s, p);
+template <typename E, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_kernel(ProductParams p) {
+  __shared__ __align__(1024) char lds[S::BYTES];
+  product<E, S, false, false>(p, blockIdx.x, lds);
+}
+
+template <typename E, typename S>
+__global__ __launch_bounds__(S::THREADS) void product_pair_kernel(PairParams q) {
+  __shared__ __align__(1024) char lds[S::BYTES];
+  uint32_t wg = blockIdx.x;
+  const uint32_t products = (uint32_t)(q.groups[0] + q.groups[1]), first = (uint32_t)(q.weight_first ? q.groups[1] : q.groups[0]);
+  if (wg < products) {
+    const bool weight = (wg < first) == (q.weight_first != 0);
+    if (wg >= first) wg -= first;
+    if (weight) product<E, S, true, true>(q.p[1], wg, lds);
+    else product<E, S, false, true>(q.p[0], wg, lds);
+    return;
+  }
+  // 16 columns of the sums, in a fixed order
+  constexpr int SLICES = S::THREADS / 16;
+  float* part = reinterpret_cast<float*>(lds);
+  const int col = threadIdx.x % 16, slice = threadIdx.x / 16;
+  const int64_t j = (int64_t)(wg - products) * 16 + col;
+  float v = 0.f;
+  if (j < q.width) {
+#pragma unroll 8
+    for (int r = slice; r < q.count; r += SLICES) v += q.partial[(int64_t)r * q.width + j];
+  }
+  part[slice * 17 + col] = v;
+  __syncthreads();
+  if (slice != 0 || j >= q.width) return;
+  v = 0.f;
+#pragma unroll
+  for (int i = 0; i < SLICES; i++) v += part[i * 17 + col];
+  q.sums[j] = v;
+}
+
+// The tiles.  Two buffers of the large one fill a unit's LDS; the small ones, whose steps are shorter than a load takes, load further ahead.
+using Tile64 = Shape<64, 64, 2, 2, 4>;
+using Tile128 = Shape<128, 128, 2, 2, 2>;
+using Tile256 = Shape<256, 256, 2, 4, 2>;
+
+template <typename E, typename S>
+hipError_t launch_one(const ProductParams& p, hipStream_t s) {
+  const int64_t tiles = ((p.I + S::TI - 1) / S::TI) * ((p.J + S::TJ - 1) / S::TJ);
+  hipLaunchKernelGGL((product_kernel<E, S>), dim3((unsigned)(tiles * p.splits)), dim3(S::THREADS), 0, s, p);
+  return hipGetLastError();
+}
+template <typename E, typename S>
+hipError_t launch_both(PairParams q, hipStream_t s) {
+  int64_t groups = 0;
+  for (int k = 0; k < 2; k++) {
+    const ProductParams& p = q.p[k];
+    if (q.groups[k] != 0) q.groups[k] = (int32_t)(((p.I + S::TI - 1) / S::TI) * ((p.J + S::TJ - 1) / S::TJ) * p.splits);
+    groups += q.groups[k];
+  }
+  q.weight_first = q.p[1].span > q.p[0].span;
+  if (q.partial != nullptr) groups += (q.width + 15) / 16;
+  hipLaunchKernelGGL((product_pair_kernel<E, S>), dim3((unsigned)groups), dim3(S::THREADS), 0, s, q);
   return hipGetLastError();
 }
 
 template <typename E>
-hipError_t launch_product(int tile, bool aa, bool ab, const ProductParams& p, hipStream_t s) {
-  if (tile == kTile256) return launch_tile<E, 256, 256, 2, 4>(aa, ab, p, s);
-  if (tile == kTile128) return launch_tile<E, 128, 128, 2, 2>(aa, ab, p, s);
-  return launch_tile<E, 64, 64, 2, 2>(aa, ab, p, s);
+hipError_t launch_product(int tile, const ProductParams& p, hipStream_t s) {
+  if (tile == kTile256) return launch_one<E, Tile256>(p, s);
+  if (tile == kTile128) return launch_one<E, Tile128>(p, s);
+  return launch_one<E, Tile64>(p, s);
+}
+template <typename E>
+hipError_t launch_pair(int tile, const PairParams& p, hipStream_t s) {
+  if (tile == kTile256) return launch_both<E, Tile256>(p, s);
+  if (tile == kTile128) return launch_both<E, Tile128>(p, s);
+  return launch_both<E, Tile64>(p, s);
 }
 
 }  // namespace linear
