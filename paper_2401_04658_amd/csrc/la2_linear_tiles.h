@@ -230,17 +230,30 @@ __device__ __forceinline__ void product(const ProductParams& p, uint32_t wg, cha
     lds_barrier();   // everybody's have, and nobody reads the buffer of the step before any more
     if (t + STAGES - 1 < steps) load(next);
     const char* tile = lds + here * STAGE;
+    // A group's operands are read while the group before it is multiplied, in that order of issue: left to itself the compiler reads
+    // right in front of the products (16384 x 8192 x 2048, the weight's gradient: 453 us so, 436 in this order)
+    Frag<E> fa[2][NI], fb[2][NJ];
+    auto fetch = [&](int g) {
+#pragma unroll
+      for (int j = 0; j < NJ; j++) fb[g & 1][j] = read<E, TJ, AB>(tile + A::BYTES, wj * NJ + j, g, lane);
+#pragma unroll
+      for (int i = 0; i < NI; i++) fa[g & 1][i] = read<E, TI, AA>(tile, wi * NI + i, g, lane);
+    };
+    constexpr int READS = NI * (AA ? 2 : 1) + NJ * (AB ? 2 : 1);   // instructions of a 16-bit group
+    fetch(0);
 #pragma unroll
     for (int g = 0; g < GROUPS; g++) {
-      Frag<E> fa[NI], fb[NJ];
-#pragma unroll
-      for (int i = 0; i < NI; i++) fa[i] = read<E, TI, AA>(tile, wi * NI + i, g, lane);
-#pragma unroll
-      for (int j = 0; j < NJ; j++) fb[j] = read<E, TJ, AB>(tile + A::BYTES, wj * NJ + j, g, lane);
+      if (g + 1 < GROUPS) fetch(g + 1);
 #pragma unroll
       for (int i = 0; i < NI; i++)
 #pragma unroll
-        for (int j = 0; j < NJ; j++) acc[i][j] = multiply<E>(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < NJ; j++) acc[i][j] = multiply<E>(fb[g & 1][j], fa[g & 1][i], acc[i][j]);
+      if (sizeof(E) == 2) {
+        constexpr int kLdsReads = 0x100, kProducts = 0x8;
+        if (g == 0) __builtin_amdgcn_sched_group_barrier(kLdsReads, READS, 0);
+        if (g + 1 < GROUPS) __builtin_amdgcn_sched_group_barrier(kLdsReads, READS, 0);
+        __builtin_amdgcn_sched_group_barrier(kProducts, NI * NJ, 0);
+      }
     }
     here = here + 1 == STAGES ? 0 : here + 1;
     next = next + 1 == STAGES ? 0 : next + 1;
