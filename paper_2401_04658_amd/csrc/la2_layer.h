@@ -46,15 +46,68 @@ struct Piece {
     for (int i = 0; i < N; i++) v[i] = (float)u[i];
   }
   static __device__ __forceinline__ void store(T* row, int at, int width, const float (&v)[N]) {
+    vec u;
+#pragma unroll
+    for (int i = 0; i < N; i++) u[i] = (T)v[i];
     if (at + N <= width) {
-      vec u;
+      *reinterpret_cast<at_element*>(row + at) = u;
+    } else if (at < width) {   // halves, quarters, ... of what is left
+      typedef unsigned __int128 bits;
+      bits b = __builtin_bit_cast(bits, u);
+      const int left = width - at;
+      T* to = row + at;
+#pragma unroll
+      for (int n = N / 2; n > 0; n >>= 1) {
+        if (left & n) {
+          typedef uint64_t u64 __attribute__((aligned(2)));
+          typedef uint32_t u32 __attribute__((aligned(2)));
+          if (n * sizeof(T) == 8) *reinterpret_cast<u64*>(to) = (uint64_t)b;
+          else if (n * sizeof(T) == 4) *reinterpret_cast<u32*>(to) = (uint32_t)b;
+          else *reinterpret_cast<uint16_t*>(to) = (uint16_t)b;
+          b >>= 8 * (int)sizeof(T) * n;
+          to += n;
+        }
+      }
+    }
+  }
+};
+
+// A lane's piece of rows of one width (a piece at least), fetched in one step and made up in another, so that the load can be under way in
+// between.  Lanes behind the row's end and the one across it load what is there: a branch around a load would make the loads behind
+// it wait (rows of 200 bf16 features, backward: 342 us with one, 165 without).  RAGGED: rows that are no whole pieces long.
+template <typename T, bool RAGGED>
+struct RowPiece {
+  using P = Piece<T>;
+  static constexpr int N = P::N;
+  int at, width;
+  __device__ __forceinline__ RowPiece(int at_, int width_) : at(at_), width(width_) {}
+  __device__ __forceinline__ typename P::vec fetch(const T* row) const {
+    return *reinterpret_cast<const typename P::at_element*>(row + min(at, width - N));
+  }
+  __device__ __forceinline__ typename P::vec settle(typename P::vec u) const {
+    typedef unsigned __int128 bits;
+    if (!RAGGED) {
+      typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+      u32x4 b = __builtin_bit_cast(u32x4, u);
+#pragma unroll
+      for (int i = 0; i < 4; i++) b[i] = at < width ? b[i] : 0;
+      return __builtin_bit_cast(typename P::vec, b);
+    }
+    if (at + N > width) {
+      bits b = __builtin_bit_cast(bits, u);
+      b = at < width ? b >> (8 * (int)sizeof(T) * (at + N - width)) : 0;
+      u = __builtin_bit_cast(typename P::vec, b);
+    }
+    return u;
+  }
+  __device__ __forceinline__ void store(T* row, const float (&v)[N]) const {
+    if (RAGGED) {
+      P::store(row, at, width, v);
+    } else if (at < width) {
+      typename P::vec u;
 #pragma unroll
       for (int i = 0; i < N; i++) u[i] = (T)v[i];
-      *reinterpret_cast<at_element*>(row + at) = u;
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; i++)
-        if (at + i < width) row[at + i] = (T)v[i];
+      *reinterpret_cast<typename P::at_element*>(row + at) = u;
     }
   }
 };
@@ -68,8 +121,8 @@ __device__ __forceinline__ T renewed(T x) {
 }
 
 // N floats of a vector of `width` from element `at` (a multiple of 4) on, `other` behind its end and for a vector that is not given.  The
-// vector starts at a multiple of 16 bytes.
-template <int N>
+// vector starts at a multiple of 16 bytes.  WHOLE: its width is a multiple of N, as `at` is.
+template <int N, bool WHOLE = false>
 __device__ __forceinline__ void load_floats(const float* p, int64_t at, int64_t width, float other, float (&v)[N]) {
   typedef __attribute__((ext_vector_type(4))) float f4;
   if (p != nullptr && at + N <= width) {
@@ -81,7 +134,7 @@ __device__ __forceinline__ void load_floats(const float* p, int64_t at, int64_t 
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = p != nullptr && at + i < width ? p[at + i] : other;
+    for (int i = 0; i < N; i++) v[i] = !WHOLE && p != nullptr && at + i < width ? p[at + i] : other;
   }
 }
 

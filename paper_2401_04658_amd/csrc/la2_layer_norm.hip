@@ -40,7 +40,7 @@ __device__ __forceinline__ float2 row_sum(float a, float b, float2* red) {
   return make_float2(a, b);
 }
 
-template <typename T, int TPR, int CH>
+template <typename T, int TPR, int CH, bool RAGGED>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(LayerNormParams p) {
   constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
@@ -48,37 +48,41 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
   float w[CH][N], b[CH][N];
 #pragma unroll
   for (int c = 0; c < CH; c++) {
-    load_floats(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
-    load_floats(p.bias, (c * TPR + lane) * N, p.width, 0.f, b[c]);
+    load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
+    load_floats<N, !RAGGED>(p.bias, (c * TPR + lane) * N, p.width, 0.f, b[c]);
   }
   const float width = (float)p.width;   // divided by, so that the mean of equal numbers is that number
   for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
-    const int end = renewed(p.width);   // the masks of a ragged end are formed for every row: kept, they overflow the scalar registers
+    const int end = RAGGED ? renewed(p.width) : p.width;   // a ragged end's masks are formed for every row: kept, they overflow the scalar registers
+    typename Piece<T>::vec raw[CH];
+#pragma unroll
+    for (int c = 0; c < CH; c++) raw[c] = RowPiece<T, RAGGED>((c * TPR + lane) * N, end).fetch(x);
     float v[CH][N], s = 0.f, q = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      Piece<T>::load(x, (c * TPR + lane) * N, end, v[c]);
+      const auto u = RowPiece<T, RAGGED>((c * TPR + lane) * N, end).settle(raw[c]);
 #pragma unroll
-      for (int i = 0; i < N; i++) s += v[c][i];
+      for (int i = 0; i < N; i++) {
+        v[c][i] = (float)u[i];
+        s += v[c][i];
+      }
     }
     const float mean = row_sum<TPR>(s, 0.f, red[0]).x / width;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const int at = (c * TPR + lane) * N;
-      if (at + N <= end) {
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-          v[c][i] -= mean;
-          q = fmaf(v[c][i], v[c][i], q);
-        }
-      } else {
+      for (int i = 0; i < N; i++) v[c][i] -= mean;
+      if (!RAGGED) {
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-          v[c][i] = at + i < end ? v[c][i] - mean : 0.f;
-          q = fmaf(v[c][i], v[c][i], q);
-        }
+        for (int i = 0; i < N; i++) v[c][i] = at < end ? v[c][i] : 0.f;
+      } else if (at + N > end) {
+#pragma unroll
+        for (int i = 0; i < N; i++) v[c][i] = at + i < end ? v[c][i] : 0.f;
       }
+#pragma unroll
+      for (int i = 0; i < N; i++) q = fmaf(v[c][i], v[c][i], q);
     }
     const float rstd = 1.f / sqrtf(row_sum<TPR>(q, 0.f, red[1]).x / width + p.eps);
     T* y = static_cast<T*>(p.y) + row * p.stride;
@@ -86,7 +90,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
     for (int c = 0; c < CH; c++) {
 #pragma unroll
       for (int i = 0; i < N; i++) v[c][i] = fmaf(v[c][i] * rstd, w[c][i], b[c][i]);
-      Piece<T>::store(y, (c * TPR + lane) * N, end, v[c]);
+      RowPiece<T, RAGGED>((c * TPR + lane) * N, end).store(y, v[c]);
     }
     if (lane == 0) {
       p.mean[row] = mean;
@@ -97,7 +101,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
 
 // TPR lanes, the columns' sums of dw (x) and db (y) of a workgroup's rows: to d_weight / d_bias where it is the only workgroup, else
 // to its row of partial
-template <typename T, int TPR, int CH>
+template <typename T, int TPR, int CH, bool RAGGED, bool SUMS>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(LayerNormParams p) {
   constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
@@ -108,7 +112,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   float w[CH][N], aw[CH][N], ab[CH][N];
 #pragma unroll
   for (int c = 0; c < CH; c++) {
-    if (KEEP) load_floats(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
+    if (KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
 #pragma unroll
     for (int i = 0; i < N; i++) aw[c][i] = ab[c][i] = 0.f;
   }
@@ -120,13 +124,14 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   const int64_t step = (int64_t)gridDim.x * RPB;
   auto fetch = [&](int64_t row) {
     if (row >= p.rows) return;
-    const int end = renewed(p.width);
+    const int end = RAGGED ? renewed(p.width) : p.width;
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
     const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      nx[c] = Piece<T>::raw(x, (c * TPR + lane) * N, end);
-      ng[c] = Piece<T>::raw(dy, (c * TPR + lane) * N, end);
+      const RowPiece<T, RAGGED> piece((c * TPR + lane) * N, end);
+      nx[c] = piece.fetch(x);
+      ng[c] = piece.fetch(dy);
     }
     next_mean = p.mean[row];
     next_rstd = p.rstd[row];
@@ -134,11 +139,12 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   fetch(row);
   for (; row < p.rows; row += step, turn ^= 1) {
-    const int end = renewed(p.width);
+    const int end = RAGGED ? renewed(p.width) : p.width;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      rx[c] = nx[c];
-      rg[c] = ng[c];
+      const RowPiece<T, RAGGED> piece((c * TPR + lane) * N, end);
+      rx[c] = piece.settle(nx[c]);
+      rg[c] = piece.settle(ng[c]);
     }
     mean = next_mean;
     rstd = next_rstd;
@@ -146,18 +152,21 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
     float sg = 0.f, sh = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      if (!KEEP) load_floats(p.weight, (c * TPR + lane) * N, end, 1.f, w[c]);
+      if (!KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, end, 1.f, w[c]);
 #pragma unroll
       for (int i = 0; i < N; i++) {   // behind the row's end dy is 0, and h finite in a row that is
         const float h = ((float)rx[c][i] - mean) * rstd, d = (float)rg[c][i], g = d * w[c][i];
-        aw[c][i] = fmaf(d, h, aw[c][i]);
-        ab[c][i] += d;
+        if (SUMS) {
+          aw[c][i] = fmaf(d, h, aw[c][i]);
+          ab[c][i] += d;
+        }
         sg += g;
         sh = fmaf(g, h, sh);
       }
     }
     const float2 s = row_sum<TPR>(sg, sh, red[turn]);
     const float mg = s.x / width, mh = s.y / width;
+    const int last = RAGGED ? renewed(p.width) : p.width;
     T* dx = static_cast<T*>(p.y) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
@@ -165,15 +174,15 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
         rx[c] = renewed(rx[c]);
         rg[c] = renewed(rg[c]);
       }
-      if (!KEEP) load_floats(p.weight, (c * TPR + lane) * N, renewed(end), 1.f, w[c]);
+      if (!KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, last, 1.f, w[c]);
       float v[N];
 #pragma unroll
       for (int i = 0; i < N; i++) v[i] = rstd * ((float)rg[c][i] * w[c][i] - mg - ((float)rx[c][i] - mean) * rstd * mh);
-      Piece<T>::store(dx, (c * TPR + lane) * N, end, v);
+      RowPiece<T, RAGGED>((c * TPR + lane) * N, last).store(dx, v);
     }
     if (!AHEAD) fetch(row + step);
   }
-  if (p.d_weight == nullptr && p.d_bias == nullptr) return;
+  if (!SUMS || (p.d_weight == nullptr && p.d_bias == nullptr)) return;
   const bool only = gridDim.x == 1;
   float* ow = only ? p.d_weight : p.partial + (int64_t)blockIdx.x * 2 * p.width;
   float* ob = only ? p.d_bias : p.partial + ((int64_t)blockIdx.x * 2 + 1) * p.width;
@@ -212,18 +221,33 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
 constexpr int kWideThreads = 1024;
 template <typename T>
 __global__ __launch_bounds__(kWideThreads) void layer_norm_wide_fwd_kernel(LayerNormParams p) {
+  constexpr int N = Piece<T>::N;
   __shared__ float2 red[2][kWideThreads / 64];
   const float width = (float)p.width;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
-    float s = 0.f, q = 0.f;
-    for (int j = threadIdx.x; j < p.width; j += kWideThreads) s += (float)x[j];
-    const float mean = row_sum<kWideThreads>(s, 0.f, red[0]).x / width;
-    for (int j = threadIdx.x; j < p.width; j += kWideThreads) q = fmaf((float)x[j] - mean, (float)x[j] - mean, q);
-    const float rstd = 1.f / sqrtf(row_sum<kWideThreads>(q, 0.f, red[1]).x / width + p.eps);
     T* y = static_cast<T*>(p.y) + row * p.stride;
-    for (int j = threadIdx.x; j < p.width; j += kWideThreads)
-      y[j] = (T)fmaf(((float)x[j] - mean) * rstd, p.weight != nullptr ? p.weight[j] : 1.f, p.bias != nullptr ? p.bias[j] : 0.f);
+    float s = 0.f, q = 0.f, v[N], w[N], b[N];
+    for (int j = threadIdx.x * N; j < p.width; j += kWideThreads * N) {
+      Piece<T>::load(x, j, p.width, v);
+#pragma unroll
+      for (int i = 0; i < N; i++) s += v[i];
+    }
+    const float mean = row_sum<kWideThreads>(s, 0.f, red[0]).x / width;
+    for (int j = threadIdx.x * N; j < p.width; j += kWideThreads * N) {
+      Piece<T>::load(x, j, p.width, v);
+#pragma unroll
+      for (int i = 0; i < N; i++) q = j + i < p.width ? fmaf(v[i] - mean, v[i] - mean, q) : q;
+    }
+    const float rstd = 1.f / sqrtf(row_sum<kWideThreads>(q, 0.f, red[1]).x / width + p.eps);
+    for (int j = threadIdx.x * N; j < p.width; j += kWideThreads * N) {
+      Piece<T>::load(x, j, p.width, v);
+      load_floats(p.weight, j, p.width, 1.f, w);
+      load_floats(p.bias, j, p.width, 0.f, b);
+#pragma unroll
+      for (int i = 0; i < N; i++) v[i] = fmaf((v[i] - mean) * rstd, w[i], b[i]);
+      Piece<T>::store(y, j, p.width, v);
+    }
     if (threadIdx.x == 0) {
       p.mean[row] = mean;
       p.rstd[row] = rstd;
@@ -233,51 +257,90 @@ __global__ __launch_bounds__(kWideThreads) void layer_norm_wide_fwd_kernel(Layer
 
 template <typename T>
 __global__ __launch_bounds__(kWideThreads) void layer_norm_wide_bwd_kernel(LayerNormParams p) {
+  constexpr int N = Piece<T>::N;
   __shared__ float2 red[2][kWideThreads / 64];
   const float width = (float)p.width;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
     const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
+    T* dx = static_cast<T*>(p.y) + row * p.stride;
     const float mean = p.mean[row], rstd = p.rstd[row];
-    float sg = 0.f, sh = 0.f;
-    for (int j = threadIdx.x; j < p.width; j += kWideThreads) {
-      const float g = (float)dy[j] * (p.weight != nullptr ? p.weight[j] : 1.f);
-      sg += g;
-      sh = fmaf(g, ((float)x[j] - mean) * rstd, sh);
+    float sg = 0.f, sh = 0.f, h[N], g[N], w[N];
+    for (int j = threadIdx.x * N; j < p.width; j += kWideThreads * N) {
+      Piece<T>::load(x, j, p.width, h);
+      Piece<T>::load(dy, j, p.width, g);
+      load_floats(p.weight, j, p.width, 1.f, w);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        sg += g[i] * w[i];
+        sh = fmaf(g[i] * w[i], (h[i] - mean) * rstd, sh);
+      }
     }
     const float2 s = row_sum<kWideThreads>(sg, sh, red[turn]);
-    T* dx = static_cast<T*>(p.y) + row * p.stride;
-    for (int j = threadIdx.x; j < p.width; j += kWideThreads) {
-      const float g = (float)dy[j] * (p.weight != nullptr ? p.weight[j] : 1.f);
-      dx[j] = (T)(rstd * (g - s.x / width - ((float)x[j] - mean) * rstd * (s.y / width)));
+    for (int j = threadIdx.x * N; j < p.width; j += kWideThreads * N) {
+      Piece<T>::load(x, j, p.width, h);
+      Piece<T>::load(dy, j, p.width, g);
+      load_floats(p.weight, j, p.width, 1.f, w);
+#pragma unroll
+      for (int i = 0; i < N; i++) g[i] = rstd * (g[i] * w[i] - s.x / width - (h[i] - mean) * rstd * (s.y / width));
+      Piece<T>::store(dx, j, p.width, g);
     }
   }
 }
 
-// ... and their columns' sums: workgroup (x, y) sums 256 columns over every gridDim.y-th row
+// ... and their columns' sums: workgroup (x, y) sums 32 pieces of columns over every gridDim.y-th group of 8 rows
+constexpr int kWideCols = 32, kWideRows = 8;
 template <typename T>
-__global__ __launch_bounds__(256) void layer_norm_wide_columns_kernel(LayerNormParams p) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= p.width) return;
-  float aw = 0.f, ab = 0.f;
-  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    const float g = (float)static_cast<const T*>(p.dy)[row * p.stride + j];
-    aw = fmaf(g, ((float)static_cast<const T*>(p.x)[row * p.stride + j] - p.mean[row]) * p.rstd[row], aw);
-    ab += g;
+__global__ __launch_bounds__(kWideCols * kWideRows) void layer_norm_wide_columns_kernel(LayerNormParams p) {
+  constexpr int N = Piece<T>::N;
+  __shared__ float2 part[kWideRows][kWideCols * N + 1];
+  const int lane = threadIdx.x % kWideCols, sub = threadIdx.x / kWideCols, first = blockIdx.x * kWideCols * N, at = first + lane * N;
+  float aw[N], ab[N];
+#pragma unroll
+  for (int i = 0; i < N; i++) aw[i] = ab[i] = 0.f;
+  if (at < p.width) {
+#pragma unroll 2
+    for (int64_t row = (int64_t)blockIdx.y * kWideRows + sub; row < p.rows; row += (int64_t)gridDim.y * kWideRows) {
+      const float mean = p.mean[row], rstd = p.rstd[row];
+      float h[N], g[N];
+      Piece<T>::load(static_cast<const T*>(p.x) + row * p.stride, at, p.width, h);
+      Piece<T>::load(static_cast<const T*>(p.dy) + row * p.stride, at, p.width, g);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        aw[i] = fmaf(g[i], (h[i] - mean) * rstd, aw[i]);
+        ab[i] += g[i];
+      }
+    }
   }
-  p.partial[(int64_t)blockIdx.y * 2 * p.width + j] = aw;
-  p.partial[((int64_t)blockIdx.y * 2 + 1) * p.width + j] = ab;
+#pragma unroll
+  for (int i = 0; i < N; i++) part[sub][lane * N + i] = make_float2(aw[i], ab[i]);
+  __syncthreads();
+  for (int c = threadIdx.x; c < kWideCols * N && first + c < p.width; c += kWideCols * kWideRows) {
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int r = 0; r < kWideRows; r++) {
+      a += part[r][c].x;
+      b += part[r][c].y;
+    }
+    p.partial[(int64_t)blockIdx.y * 2 * p.width + first + c] = a;
+    p.partial[((int64_t)blockIdx.y * 2 + 1) * p.width + first + c] = b;
+  }
 }
 
 template <int TPR, int CH>
 struct Split {
   static constexpr int tpr = TPR, ch = CH;
+  // backward: so many elements of a row do not fit the registers beside their columns' sums, which are then formed in a pass of their
+  // own (8192 rows of 16384 bf16 features: 370 us with the sums in scratch memory, 279 so)
+  template <typename T>
+  static constexpr bool apart = TPR == 0 || TPR > 512 || CH * Piece<T>::N > 16;
 };
-// Calls f(Split) for the lanes and pieces of a row of `width`, f(Split<0, 0>) where no split holds it.
+// Calls f(Split) for the lanes and pieces of a row of `width`, f(Split<0, 0>) where no split holds it or it is less than a piece.
 template <typename T, bool BWD, typename F>
 auto split_of(int32_t width, F f) {
   const int pieces = (width + Piece<T>::N - 1) / Piece<T>::N;
+  if (width < Piece<T>::N) return f(Split<0, 0>{});
   if (pieces <= 8) return f(Split<8, 1>{});
   if (pieces <= 16) return f(Split<16, 1>{});
   if (pieces <= 32) return f(Split<32, 1>{});
@@ -289,11 +352,9 @@ auto split_of(int32_t width, F f) {
     if (pieces <= 256) return f(Split<256, 1>{});
   if (pieces <= 512) return f(Split<256, 2>{});
   if (pieces <= 1024) return f(Split<512, 2>{});
-  if constexpr (BWD && sizeof(T) == 2) {   // 32 elements a lane do not fit the registers beside their sums
-    if (pieces <= 2048) return f(Split<1024, 2>{});
-  } else {
-    if (pieces <= 2048) return f(Split<512, 4>{});
-  }
+  if (pieces <= 2048) return f(Split<512, 4>{});
+  if constexpr (sizeof(T) == 4)
+    if (pieces <= 4096) return f(Split<1024, 4>{});
   return f(Split<0, 0>{});
 }
 
@@ -306,6 +367,12 @@ int64_t groups(int64_t rows, int units, int most) {
 }
 constexpr int kFwdPerUnit = 8, kBwdPerUnit = 2;
 
+template <typename S, typename K>
+void launch_rows(const LayerNormParams& p, int units, int most, hipStream_t s, K whole, K ragged, int piece) {
+  hipLaunchKernelGGL(p.width % piece == 0 ? whole : ragged, dim3((unsigned)groups<S::tpr>(p.rows, units, most)), dim3(Shape<S::tpr>::kThreads), 0,
+                     s, p);
+}
+
 template <typename T>
 hipError_t fwd(const LayerNormParams& p, int units, hipStream_t s) {
   return split_of<T, false>(p.width, [&](auto split) {
@@ -313,8 +380,8 @@ hipError_t fwd(const LayerNormParams& p, int units, hipStream_t s) {
     if constexpr (S::tpr == 0)
       hipLaunchKernelGGL(layer_norm_wide_fwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
     else
-      hipLaunchKernelGGL((layer_norm_fwd_kernel<T, S::tpr, S::ch>), dim3((unsigned)groups<S::tpr>(p.rows, units, kFwdPerUnit)),
-                         dim3(Shape<S::tpr>::kThreads), 0, s, p);
+      launch_rows<S>(p, units, kFwdPerUnit, s, layer_norm_fwd_kernel<T, S::tpr, S::ch, false>, layer_norm_fwd_kernel<T, S::tpr, S::ch, true>,
+                     Piece<T>::N);
     return hipGetLastError();
   });
 }
@@ -323,7 +390,7 @@ template <typename T>
 int64_t partials(int64_t rows, int32_t width, int units) {
   return split_of<T, true>(width, [&](auto split) -> int64_t {
     using S = decltype(split);
-    if constexpr (S::tpr == 0) return rows < 1 ? 1 : rows < 64 ? rows : 64;
+    if constexpr (S::template apart<T>) return rows < 1 ? 1 : rows < 64 * kWideRows ? (rows + kWideRows - 1) / kWideRows : 64;
     const int64_t g = groups<S::tpr == 0 ? 64 : S::tpr>(rows, units, kBwdPerUnit);
     return g > 1 ? g : 0;
   });
@@ -335,14 +402,15 @@ hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
   const int64_t count = partials<T>(p.rows, p.width, units);
   hipError_t e = split_of<T, true>(p.width, [&](auto split) {
     using S = decltype(split);
-    if constexpr (S::tpr == 0) {
-      if (sums)   // first: dx may take dy's place
-        hipLaunchKernelGGL(layer_norm_wide_columns_kernel<T>, dim3((unsigned)((p.width + 255) / 256), (unsigned)count), dim3(256), 0, s, p);
+    constexpr bool APART = S::template apart<T>;
+    if (APART && sums)   // first: dx may take dy's place
+      hipLaunchKernelGGL(layer_norm_wide_columns_kernel<T>, dim3((unsigned)((p.width + kWideCols * Piece<T>::N - 1) / (kWideCols * Piece<T>::N)), (unsigned)count),
+                         dim3(kWideCols * kWideRows), 0, s, p);
+    if constexpr (S::tpr == 0)
       hipLaunchKernelGGL(layer_norm_wide_bwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
-    } else {
-      hipLaunchKernelGGL((layer_norm_bwd_kernel<T, S::tpr, S::ch>), dim3((unsigned)groups<S::tpr>(p.rows, units, kBwdPerUnit)),
-                         dim3(Shape<S::tpr>::kThreads), 0, s, p);
-    }
+    else
+      launch_rows<S>(p, units, kBwdPerUnit, s, layer_norm_bwd_kernel<T, S::tpr, S::ch, false, !APART>,
+                     layer_norm_bwd_kernel<T, S::tpr, S::ch, true, !APART>, Piece<T>::N);
     return hipGetLastError();
   });
   if (e != hipSuccess || !sums || count == 0) return e;
