@@ -41,15 +41,28 @@ __device__ __forceinline__ uint64_t key_of(float x, int token) {
   return x == -INFINITY ? 0 : (uint64_t)ordered(x + 0.f) << 32 | (0xFFFFFFFFu - (uint32_t)token);
 }
 
+// How many of `have` values are larger than the one that larger(k) compares with value k: eight lanes count together.
+constexpr int kRankLanes = 8;
+template <typename F>
+__device__ __forceinline__ int rank_of(int have, F larger) {
+  int n = 0;
+#pragma unroll 2
+  for (int k = threadIdx.x % kRankLanes; k < have; k += kRankLanes) n += larger(k);
+#pragma unroll
+  for (int k = 1; k < kRankLanes; k <<= 1) n += __shfl_xor(n, k);
+  return n;
+}
+
 __device__ __forceinline__ int votes(bool yes) { return __popcll(__ballot(yes)); }
 
 // The largest T that at least n of the `in` lanes' words reach (0 if there are fewer than n), or a smaller one that exactly n reach.
 __device__ __forceinline__ uint32_t nth_word(uint32_t word, bool in, int n) {
   uint32_t t = 0;
-  for (int bit = 31; bit >= 0; bit--) {
-    const uint32_t c = t | 1u << bit;
-    const int reach = votes(in && word >= c);
-    if (reach >= n) t = c;
+  for (int bit = 30; bit >= 0; bit -= 2) {   // two bits at a time: the three votes do not wait for one another
+    const uint32_t one = t | 1u << bit, two = t | 2u << bit, three = t | 3u << bit;
+    const int reach1 = votes(in && word >= one), reach2 = votes(in && word >= two), reach3 = votes(in && word >= three);
+    const int reach = reach3 >= n ? reach3 : reach2 >= n ? reach2 : reach1;
+    t = reach3 >= n ? three : reach2 >= n ? two : reach1 >= n ? one : t;
     if (reach == n) break;
   }
   return t;
@@ -90,18 +103,26 @@ __global__ __launch_bounds__(kSelectThreads) void beam_chunk_kernel(BeamSelectPa
   int kept = 0;
   for (int first = begin; first < end; first += PART) {
     float v[P][N], m = -INFINITY, second = -INFINITY;   // a thread's largest two
+    typename Piece<T>::vec raw[P];
+    if (p.vocab >= N) {
 #pragma unroll
-    for (int c = 0; c < P; c++) Piece<T>::load(x, first + (c * kSelectThreads + tid) * N, p.vocab, v[c]);
+      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, true>(first + (c * kSelectThreads + tid) * N, p.vocab).fetch(x);
+#pragma unroll
+      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, true>(first + (c * kSelectThreads + tid) * N, p.vocab).settle(raw[c]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < P; c++) raw[c] = Piece<T>::raw(x, first + (c * kSelectThreads + tid) * N, p.vocab);
+    }
     if (tid == 0) count = 0;
 #pragma unroll
     for (int c = 0; c < P; c++) {
       const int at = first + (c * kSelectThreads + tid) * N;
       if (at + N <= p.vocab) {
 #pragma unroll
-        for (int i = 0; i < N; i++) v[c][i] = clean_logit(v[c][i]);
+        for (int i = 0; i < N; i++) v[c][i] = clean_logit((float)raw[c][i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < N; i++) v[c][i] = at + i < p.vocab ? clean_logit(v[c][i]) : -INFINITY;
+        for (int i = 0; i < N; i++) v[c][i] = at + i < p.vocab ? clean_logit((float)raw[c][i]) : -INFINITY;
       }
 #pragma unroll
       for (int i = 0; i < N; i++) {
@@ -165,12 +186,10 @@ __global__ __launch_bounds__(kSelectThreads) void beam_chunk_kernel(BeamSelectPa
       if (tid < kept) found[fresh + tid] = best_of[tid];
       __syncthreads();
       const int have = fresh + kept;
-      for (int c = tid; c < have; c += kSelectThreads) {
+      for (int c = tid / kRankLanes; c < have; c += kSelectThreads / kRankLanes) {
         const uint64_t key = found[c];
-        int larger = 0;
-#pragma unroll 4
-        for (int k = 0; k < have; k++) larger += found[k] > key;
-        if (larger < n) best_of[larger] = key;
+        const int rank = rank_of(have, [&](int k) { return found[k] > key; });
+        if (rank < n && tid % kRankLanes == 0) best_of[rank] = key;
       }
       kept = min(n, have);
     } else {   // one after the other
@@ -214,8 +233,11 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
   __shared__ float start[kMaxBeams];
   __shared__ int kind[kMaxBeams];                          // 0: no candidates, 1: its vocabulary, 2: finished, one candidate
   __shared__ uint32_t bounds[WAVES][3];
-  __shared__ uint64_t found_score[kMaxBeams * WAVES * KPT];   // at most n lanes a wave hold any
-  __shared__ uint32_t found_place[kMaxBeams * WAVES * KPT];
+  struct __align__(16) Scored {
+    uint64_t score;
+    uint32_t place;
+  };
+  __shared__ Scored found[kMaxBeams * WAVES * KPT];   // at most n lanes a wave hold any
   __shared__ int count;
   const int n = p.beams, tid = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * n;
@@ -224,7 +246,8 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
 #pragma unroll
   for (int k = 0; k < KPT; k++) {   // (those of finished and dead beams were not written and are not used)
     const int c = tid + k * THREADS;
-    key[k] = c < total ? p.keys[row0 * per + c] : 0;
+    const uint64_t there = p.keys[row0 * per + min(c, total - 1)];   // (no branch: the loads are all under way together)
+    key[k] = c < total ? there : 0;
   }
   if (tid < 8 * kMaxBeams) {   // eight lanes a beam
     const int beam = tid / 8, lane = tid % 8;
@@ -295,8 +318,7 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
   for (int k = 0; k < KPT; k++)
     if (score[k] != 0 && (score[k] > bound || (score[k] == bound && place[k] >= bound_place))) {
       const int at = atomicAdd(&count, 1);
-      found_score[at] = score[k];
-      found_place[at] = place[k];
+      found[at] = Scored{score[k], place[k]};
     }
   __syncthreads();
   const int have = count;
@@ -306,15 +328,13 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
     p.token[row0 + slot] = token;
     p.out_finished[row0 + slot] = done ? 1 : 0;
   };
-  for (int c = tid; c < have; c += THREADS) {
-    const uint64_t mine = found_score[c];
-    const uint32_t at = found_place[c];
-    int larger = 0;
-#pragma unroll 4
-    for (int k = 0; k < have; k++) larger += found_score[k] > mine || (found_score[k] == mine && found_place[k] > at);
-    if (larger < n) {
-      const int parent = (int)(~at / (uint32_t)p.vocab), token = (int)(~at % (uint32_t)p.vocab);
-      write(larger, (float)from_ordered(mine), parent, token, kind[parent] == 2 || token == p.eos);
+  for (int c = tid / kRankLanes; c < have; c += THREADS / kRankLanes) {
+    const Scored mine = found[c];
+    const int rank = rank_of(have, [&](int k) { return found[k].score > mine.score || (found[k].score == mine.score && found[k].place > mine.place); });
+    if (rank < n && tid % kRankLanes == 0) {
+      const uint32_t place = ~mine.place;
+      const int parent = (int)(place / (uint32_t)p.vocab), token = (int)(place % (uint32_t)p.vocab);
+      write(rank, (float)from_ordered(mine.score), parent, token, kind[parent] == 2 || token == p.eos);
     }
   }
   for (int c = have + tid; c < n; c += THREADS) write(c, -INFINITY, c, p.eos >= 0 ? p.eos : 0, true);
@@ -352,7 +372,7 @@ __global__ __launch_bounds__(kReorderThreads) void beam_reorder_kernel(BeamReord
 
 // How the vocabulary is cut.  Pieces of 4096 logits, or 8192 where the rows alone fill the device; a workgroup works off several where their
 // candidates would be more than the second launch's threads hold.
-constexpr int kSmallPart = 4096, kLargePart = 8192, kMergeMost = 1024 * 8, kMergeFew = 256 * 4;
+constexpr int kSmallPart = 4096, kLargePart = 8192, kMergeMost = 1024 * 8, kMergeMore = 512 * 4, kMergeFew = 256 * 4;
 static_assert(kMaxBeams * kMaxBeams <= kMergeMost, "one piece a row at least");
 
 struct Cut {
@@ -375,7 +395,9 @@ hipError_t select(BeamSelectParams p, const Cut& c, hipStream_t s) {
   else hipLaunchKernelGGL((beam_chunk_kernel<T, kLarge>), grid, dim3(kSelectThreads), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.beams * p.beams * p.chunks <= kMergeFew) hipLaunchKernelGGL((beam_merge_kernel<256, 4>), dim3((unsigned)p.batch), dim3(256), 0, s, p);
+  const int candidates = p.beams * p.beams * p.chunks;
+  if (candidates <= kMergeFew) hipLaunchKernelGGL((beam_merge_kernel<256, 4>), dim3((unsigned)p.batch), dim3(256), 0, s, p);
+  else if (candidates <= kMergeMore) hipLaunchKernelGGL((beam_merge_kernel<512, 4>), dim3((unsigned)p.batch), dim3(512), 0, s, p);
   else hipLaunchKernelGGL((beam_merge_kernel<1024, 8>), dim3((unsigned)p.batch), dim3(1024), 0, s, p);
   return hipGetLastError();
 }
