@@ -106,9 +106,9 @@ __global__ __launch_bounds__(kSelectThreads) void beam_chunk_kernel(BeamSelectPa
     typename Piece<T>::vec raw[P];
     if (p.vocab >= N) {
 #pragma unroll
-      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, true>(first + (c * kSelectThreads + tid) * N, p.vocab).fetch(x);
+      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, kRagged>(first + (c * kSelectThreads + tid) * N, p.vocab).fetch(x);
 #pragma unroll
-      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, true>(first + (c * kSelectThreads + tid) * N, p.vocab).settle(raw[c]);
+      for (int c = 0; c < P; c++) raw[c] = RowPiece<T, kRagged>(first + (c * kSelectThreads + tid) * N, p.vocab).settle(raw[c]);
     } else {
 #pragma unroll
       for (int c = 0; c < P; c++) raw[c] = Piece<T>::raw(x, first + (c * kSelectThreads + tid) * N, p.vocab);

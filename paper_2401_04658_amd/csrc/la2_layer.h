@@ -45,12 +45,14 @@ struct Piece {
 #pragma unroll
     for (int i = 0; i < N; i++) v[i] = (float)u[i];
   }
-  static __device__ __forceinline__ void store(T* row, int at, int width, const float (&v)[N]) {
+  // `past`: past the caches (whole pieces)
+  static __device__ __forceinline__ void store(T* row, int at, int width, const float (&v)[N], bool past = false) {
     vec u;
 #pragma unroll
     for (int i = 0; i < N; i++) u[i] = (T)v[i];
     if (at + N <= width) {
-      *reinterpret_cast<at_element*>(row + at) = u;
+      if (past) __builtin_nontemporal_store(u, reinterpret_cast<at_element*>(row + at));
+      else *reinterpret_cast<at_element*>(row + at) = u;
     } else if (at < width) {   // halves, quarters, ... of what is left
       typedef unsigned __int128 bits;
       bits b = __builtin_bit_cast(bits, u);
@@ -74,19 +76,21 @@ struct Piece {
 
 // A lane's piece of rows of one width (a piece at least), fetched in one step and made up in another, so that the load can be under way in
 // between.  Lanes behind the row's end and the one across it load what is there: a branch around a load would make the loads behind
-// it wait (rows of 200 bf16 features, backward: 342 us with one, 165 without).  RAGGED: rows that are no whole pieces long.
-template <typename T, bool RAGGED>
+// it wait (rows of 200 bf16 features, backward: 342 us with one, 165 without).
+enum Edge { kFits, kWhole, kRagged };   // rows that the lanes' pieces cover exactly; of whole pieces; of any length
+template <typename T, Edge EDGE>
 struct RowPiece {
   using P = Piece<T>;
   static constexpr int N = P::N;
   int at, width;
   __device__ __forceinline__ RowPiece(int at_, int width_) : at(at_), width(width_) {}
   __device__ __forceinline__ typename P::vec fetch(const T* row) const {
-    return *reinterpret_cast<const typename P::at_element*>(row + min(at, width - N));
+    return *reinterpret_cast<const typename P::at_element*>(row + (EDGE == kFits ? at : min(at, width - N)));
   }
   __device__ __forceinline__ typename P::vec settle(typename P::vec u) const {
     typedef unsigned __int128 bits;
-    if (!RAGGED) {
+    if (EDGE == kFits) return u;
+    if (EDGE == kWhole) {
       typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
       u32x4 b = __builtin_bit_cast(u32x4, u);
 #pragma unroll
@@ -101,9 +105,9 @@ struct RowPiece {
     return u;
   }
   __device__ __forceinline__ void store(T* row, const float (&v)[N]) const {
-    if (RAGGED) {
+    if (EDGE == kRagged) {
       P::store(row, at, width, v);
-    } else if (at < width) {
+    } else if (EDGE == kFits || at < width) {
       typename P::vec u;
 #pragma unroll
       for (int i = 0; i < N; i++) u[i] = (T)v[i];

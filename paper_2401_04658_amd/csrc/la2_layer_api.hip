@@ -48,7 +48,7 @@ la2_status check_linear(const la2_linear_desc* d) {
   // a tile's rows are addressed with 31-bit byte offsets, 256 rows at most
   const int64_t most = (((int64_t)1 << 23) - 1) / (d->dtype == LA2_F32 ? 4 : 2);
   if (d->stride_x > most || d->stride_w > most || d->stride_y > most) return LA2_ERR_SHAPE;
-  if (d->rows > kMostElements / (1 + (d->in_features > d->out_features ? d->in_features : d->out_features))) return LA2_ERR_SHAPE;
+  if (d->rows > INT32_MAX || d->rows > kMostElements / (1 + (d->in_features > d->out_features ? d->in_features : d->out_features))) return LA2_ERR_SHAPE;
   return LA2_OK;
 }
 la2::LinearParams linear_params(const la2_linear_desc* d) {

@@ -40,7 +40,7 @@ __device__ __forceinline__ float2 row_sum(float a, float b, float2* red) {
   return make_float2(a, b);
 }
 
-template <typename T, int TPR, int CH, bool RAGGED>
+template <typename T, int TPR, int CH, Edge EDGE>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(LayerNormParams p) {
   constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
@@ -48,20 +48,20 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
   float w[CH][N], b[CH][N];
 #pragma unroll
   for (int c = 0; c < CH; c++) {
-    load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
-    load_floats<N, !RAGGED>(p.bias, (c * TPR + lane) * N, p.width, 0.f, b[c]);
+    load_floats<N, EDGE != kRagged>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
+    load_floats<N, EDGE != kRagged>(p.bias, (c * TPR + lane) * N, p.width, 0.f, b[c]);
   }
   const float width = (float)p.width;   // divided by, so that the mean of equal numbers is that number
   for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.rows; row += (int64_t)gridDim.x * RPB) {
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
-    const int end = RAGGED ? renewed(p.width) : p.width;   // a ragged end's masks are formed for every row: kept, they overflow the scalar registers
+    const int end = EDGE == kRagged ? renewed(p.width) : p.width;   // a ragged end's masks are formed for every row: kept, they overflow the scalar registers
     typename Piece<T>::vec raw[CH];
 #pragma unroll
-    for (int c = 0; c < CH; c++) raw[c] = RowPiece<T, RAGGED>((c * TPR + lane) * N, end).fetch(x);
+    for (int c = 0; c < CH; c++) raw[c] = RowPiece<T, EDGE>((c * TPR + lane) * N, end).fetch(x);
     float v[CH][N], s = 0.f, q = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const auto u = RowPiece<T, RAGGED>((c * TPR + lane) * N, end).settle(raw[c]);
+      const auto u = RowPiece<T, EDGE>((c * TPR + lane) * N, end).settle(raw[c]);
 #pragma unroll
       for (int i = 0; i < N; i++) {
         v[c][i] = (float)u[i];
@@ -74,10 +74,10 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
       const int at = (c * TPR + lane) * N;
 #pragma unroll
       for (int i = 0; i < N; i++) v[c][i] -= mean;
-      if (!RAGGED) {
+      if (EDGE == kWhole) {
 #pragma unroll
         for (int i = 0; i < N; i++) v[c][i] = at < end ? v[c][i] : 0.f;
-      } else if (at + N > end) {
+      } else if (EDGE == kRagged && at + N > end) {
 #pragma unroll
         for (int i = 0; i < N; i++) v[c][i] = at + i < end ? v[c][i] : 0.f;
       }
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
     for (int c = 0; c < CH; c++) {
 #pragma unroll
       for (int i = 0; i < N; i++) v[c][i] = fmaf(v[c][i] * rstd, w[c][i], b[c][i]);
-      RowPiece<T, RAGGED>((c * TPR + lane) * N, end).store(y, v[c]);
+      RowPiece<T, EDGE>((c * TPR + lane) * N, end).store(y, v[c]);
     }
     if (lane == 0) {
       p.mean[row] = mean;
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_fwd_kernel(La
 
 // TPR lanes, the columns' sums of dw (x) and db (y) of a workgroup's rows: to d_weight / d_bias where it is the only workgroup, else
 // to its row of partial
-template <typename T, int TPR, int CH, bool RAGGED, bool SUMS>
+template <typename T, int TPR, int CH, Edge EDGE, bool SUMS>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(LayerNormParams p) {
   constexpr int N = Piece<T>::N, RPB = Shape<TPR>::kRows;
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   float w[CH][N], aw[CH][N], ab[CH][N];
 #pragma unroll
   for (int c = 0; c < CH; c++) {
-    if (KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
+    if (KEEP) load_floats<N, EDGE != kRagged>(p.weight, (c * TPR + lane) * N, p.width, 1.f, w[c]);
 #pragma unroll
     for (int i = 0; i < N; i++) aw[c][i] = ab[c][i] = 0.f;
   }
@@ -124,12 +124,12 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   const int64_t step = (int64_t)gridDim.x * RPB;
   auto fetch = [&](int64_t row) {
     if (row >= p.rows) return;
-    const int end = RAGGED ? renewed(p.width) : p.width;
+    const int end = EDGE == kRagged ? renewed(p.width) : p.width;
     const T* x = static_cast<const T*>(p.x) + row * p.stride;
     const T* dy = static_cast<const T*>(p.dy) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const RowPiece<T, RAGGED> piece((c * TPR + lane) * N, end);
+      const RowPiece<T, EDGE> piece((c * TPR + lane) * N, end);
       nx[c] = piece.fetch(x);
       ng[c] = piece.fetch(dy);
     }
@@ -139,10 +139,10 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   fetch(row);
   for (; row < p.rows; row += step, turn ^= 1) {
-    const int end = RAGGED ? renewed(p.width) : p.width;
+    const int end = EDGE == kRagged ? renewed(p.width) : p.width;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const RowPiece<T, RAGGED> piece((c * TPR + lane) * N, end);
+      const RowPiece<T, EDGE> piece((c * TPR + lane) * N, end);
       rx[c] = piece.settle(nx[c]);
       rg[c] = piece.settle(ng[c]);
     }
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
     float sg = 0.f, sh = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      if (!KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, end, 1.f, w[c]);
+      if (!KEEP) load_floats<N, EDGE != kRagged>(p.weight, (c * TPR + lane) * N, end, 1.f, w[c]);
 #pragma unroll
       for (int i = 0; i < N; i++) {   // behind the row's end dy is 0, and h finite in a row that is
         const float h = ((float)rx[c][i] - mean) * rstd, d = (float)rg[c][i], g = d * w[c][i];
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
     }
     const float2 s = row_sum<TPR>(sg, sh, red[turn]);
     const float mg = s.x / width, mh = s.y / width;
-    const int last = RAGGED ? renewed(p.width) : p.width;
+    const int last = EDGE == kRagged ? renewed(p.width) : p.width;
     T* dx = static_cast<T*>(p.y) + row * p.stride;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
@@ -174,11 +174,11 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
         rx[c] = renewed(rx[c]);
         rg[c] = renewed(rg[c]);
       }
-      if (!KEEP) load_floats<N, !RAGGED>(p.weight, (c * TPR + lane) * N, last, 1.f, w[c]);
+      if (!KEEP) load_floats<N, EDGE != kRagged>(p.weight, (c * TPR + lane) * N, last, 1.f, w[c]);
       float v[N];
 #pragma unroll
       for (int i = 0; i < N; i++) v[i] = rstd * ((float)rg[c][i] * w[c][i] - mg - ((float)rx[c][i] - mean) * rstd * mh);
-      RowPiece<T, RAGGED>((c * TPR + lane) * N, last).store(dx, v);
+      RowPiece<T, EDGE>((c * TPR + lane) * N, last).store(dx, v);
     }
     if (!AHEAD) fetch(row + step);
   }
@@ -368,8 +368,8 @@ int64_t groups(int64_t rows, int units, int most) {
 constexpr int kFwdPerUnit = 8, kBwdPerUnit = 2;
 
 template <typename S, typename K>
-void launch_rows(const LayerNormParams& p, int units, int most, hipStream_t s, K whole, K ragged, int piece) {
-  hipLaunchKernelGGL(p.width % piece == 0 ? whole : ragged, dim3((unsigned)groups<S::tpr>(p.rows, units, most)), dim3(Shape<S::tpr>::kThreads), 0,
+void launch_rows(const LayerNormParams& p, int units, int most, hipStream_t s, K fits, K whole, K ragged, int piece) {
+  hipLaunchKernelGGL(p.width == S::tpr * S::ch * piece ? fits : p.width % piece == 0 ? whole : ragged, dim3((unsigned)groups<S::tpr>(p.rows, units, most)), dim3(Shape<S::tpr>::kThreads), 0,
                      s, p);
 }
 
@@ -380,8 +380,8 @@ hipError_t fwd(const LayerNormParams& p, int units, hipStream_t s) {
     if constexpr (S::tpr == 0)
       hipLaunchKernelGGL(layer_norm_wide_fwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
     else
-      launch_rows<S>(p, units, kFwdPerUnit, s, layer_norm_fwd_kernel<T, S::tpr, S::ch, false>, layer_norm_fwd_kernel<T, S::tpr, S::ch, true>,
-                     Piece<T>::N);
+      launch_rows<S>(p, units, kFwdPerUnit, s, layer_norm_fwd_kernel<T, S::tpr, S::ch, kFits>, layer_norm_fwd_kernel<T, S::tpr, S::ch, kWhole>,
+                     layer_norm_fwd_kernel<T, S::tpr, S::ch, kRagged>, Piece<T>::N);
     return hipGetLastError();
   });
 }
@@ -409,8 +409,8 @@ hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
     if constexpr (S::tpr == 0)
       hipLaunchKernelGGL(layer_norm_wide_bwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
     else
-      launch_rows<S>(p, units, kBwdPerUnit, s, layer_norm_bwd_kernel<T, S::tpr, S::ch, false, !APART>,
-                     layer_norm_bwd_kernel<T, S::tpr, S::ch, true, !APART>, Piece<T>::N);
+      launch_rows<S>(p, units, kBwdPerUnit, s, layer_norm_bwd_kernel<T, S::tpr, S::ch, kFits, !APART>,
+                     layer_norm_bwd_kernel<T, S::tpr, S::ch, kWhole, !APART>, layer_norm_bwd_kernel<T, S::tpr, S::ch, kRagged, !APART>, Piece<T>::N);
     return hipGetLastError();
   });
   if (e != hipSuccess || !sums || count == 0) return e;

@@ -27,6 +27,7 @@ struct ProductParams {
   void* pre;
   int64_t ldo;
   int32_t act;
+  int32_t past;   // out and pre go past the caches: too large to be found there by what reads them next
   // The reduction cut into `splits` pieces of `span` (a multiple of the kernels' step): the pieces' sums go to partial
   // [splits][I][J] and a launch of its own joins them.  splits == 1: partial is not used.
   int32_t splits;
@@ -131,7 +132,7 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t i, int64_
   const int64_t row = i * p.ldo;
 #pragma unroll
   for (int k = 0; k < N; k++) v[k] += b[k];
-  if (p.pre != nullptr) Piece<E>::store(static_cast<E*>(p.pre) + row, (int)j, (int)p.J, v);
+  if (p.pre != nullptr) Piece<E>::store(static_cast<E*>(p.pre) + row, (int)j, (int)p.J, v, p.past != 0);
 #pragma unroll
   for (int k = 0; k < N; k++) v[k] = act_of<ACT>(v[k]);
   if (p.residual != nullptr) {
@@ -140,7 +141,7 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t i, int64_
 #pragma unroll
     for (int k = 0; k < N; k++) v[k] += r[k];
   }
-  Piece<E>::store(static_cast<E*>(p.out) + row, (int)j, (int)p.J, v);
+  Piece<E>::store(static_cast<E*>(p.out) + row, (int)j, (int)p.J, v, p.past != 0);
 }
 
 }  // namespace la2

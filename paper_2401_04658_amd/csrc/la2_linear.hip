@@ -141,11 +141,12 @@ struct PrepareParams {
 template <typename E>
 __device__ __forceinline__ void pad_rows(const PadParams& p, uint32_t wg) {
   constexpr int N = Piece<E>::N;
-  const int64_t pieces = p.ldo / N, at = (int64_t)wg * 256 + threadIdx.x;
-  if (at >= p.rows * pieces) return;
-  const int64_t row = at / pieces, col = at % pieces * N;
-  *reinterpret_cast<typename Piece<E>::vec*>(static_cast<E*>(p.to) + row * p.ldo + col) =
-      Piece<E>::raw(static_cast<const E*>(p.from) + row * p.ld, col, p.width);
+  const int64_t pieces = p.ldo / N;
+  for (int64_t at = (int64_t)wg * 256 + threadIdx.x; at < p.rows * pieces; at += (int64_t)p.groups * 256) {
+    const int64_t row = at / pieces, col = at % pieces * N;
+    *reinterpret_cast<typename Piece<E>::vec*>(static_cast<E*>(p.to) + row * p.ldo + col) =
+        Piece<E>::raw(static_cast<const E*>(p.from) + row * p.ld, col, p.width);
+  }
 }
 template <typename E>
 __global__ __launch_bounds__(kSlopeCols * kSlopeRows) void linear_prepare_kernel(PrepareParams p) {
@@ -203,6 +204,9 @@ size_t elem(int dtype) { return dtype == kF32 ? 4 : 2; }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 int64_t chunk(int dtype) { return dtype == kF32 ? 4 : 8; }   // elements of 16 bytes
 bool whole_chunks(int dtype, int64_t ld, int64_t width) { return width == 0 || (ld % chunk(dtype) == 0 && width % chunk(dtype) == 0); }
+
+// Outputs that do not fit the memory-side cache (256 MiB) are stored past the caches: 16384 x 8192 bf16 with its sums kept 547 us against 561.
+bool past_caches(int64_t rows, int64_t width, int dtype) { return rows * width * (int64_t)elem(dtype) >= (int64_t)256 << 20; }
 
 // Takes pieces of the workspace, each from a multiple of 256 bytes on; without a workspace it only counts.
 struct Taker {
@@ -313,7 +317,7 @@ void regular(int dtype, const void*& at, int64_t& ld, int64_t rows, int64_t widt
   pad.ldo = ldo;
   pad.rows = rows;
   pad.width = (int32_t)width;
-  pad.groups = (int32_t)((pieces + 255) / 256);
+  pad.groups = (int32_t)std::min<int64_t>((pieces + 255) / 256, 1 << 20);
   at = pad.to;
   ld = ldo;
 }
@@ -351,6 +355,7 @@ hipError_t forward(const LinearParams& q, Taker& t, bool count_only, int units, 
   p.pre = q.pre;
   p.ldo = q.stride_y;
   p.act = q.act;
+  p.past = past_caches(q.rows, q.out, q.dtype);
   p.splits = 1;
   if (p.I == 0 || p.J == 0) return hipSuccess;
   if (few_rows(q.rows, q.in, q.out, units)) {
@@ -410,6 +415,7 @@ hipError_t backward(const LinearParams& q, Taker& t, bool count_only, int units,
     p.b = q.w;
     p.ldb = q.stride_w;
     p.out = q.dx;
+    p.past = past_caches(q.rows, q.in, d);
     p.ldo = q.stride_x;
     regular(d, p.b, p.ldb, q.out, q.in, t, pre.pad[0]);
     e[count] = Extent{p.I, p.J, p.R};
@@ -425,6 +431,7 @@ hipError_t backward(const LinearParams& q, Taker& t, bool count_only, int units,
     p.b = q.x;
     p.ldb = q.stride_x;
     p.out = q.dw;
+    p.past = past_caches(q.out, q.in, d);
     p.ldo = q.stride_w;
     regular(d, p.b, p.ldb, q.rows, q.in, t, pre.pad[1]);
     e[count] = Extent{p.I, p.J, p.R};
