@@ -9,8 +9,8 @@ import pytest
 from paper_2401_04658_amd import build
 
 FAMILIES = {   # scratch bytes per lane, waves per SIMD at least
-    "layer_norm_fwd_kernel": (0, 2), "layer_norm_bwd_kernel": (128, 2), "layer_norm_wide_fwd_kernel": (0, 4), "layer_norm_wide_bwd_kernel": (0, 4),
-    "layer_norm_wide_columns_kernel": (0, 8), "column_sum_kernel": (0, 4), "linear_few_kernel": (0, 2), "linear_join_kernel": (0, 4),
+    "layer_norm_fwd_kernel": (0, 2), "layer_norm_bwd_kernel": (0, 2), "layer_norm_wide_fwd_kernel": (0, 4), "layer_norm_wide_bwd_kernel": (0, 4),
+    "layer_norm_wide_columns_kernel": (0, 4), "column_sum_kernel": (0, 4), "linear_few_kernel": (0, 2), "linear_join_kernel": (0, 4),
     "linear_prepare_kernel": (0, 2), "product_kernel": (0, 2), "product_pair_kernel": (0, 2), "beam_chunk_kernel": (0, 4),
     "beam_merge_kernel": (0, 2), "beam_reorder_kernel": (0, 3),
 }
@@ -41,9 +41,6 @@ def test_every_family_is_built_and_within_its_limits(resources):
         scratch, waves = FAMILIES[f]
         assert v["ScratchSize"] <= scratch and v["SGPRs_Spill"] == 0, (k, v["ScratchSize"], v["SGPRs_Spill"])
         assert v["Occupancy"] >= waves, (k, v["Occupancy"])
-        # only the 16-bit rows of 8193 to 16384 features park a few registers
-        if f == "layer_norm_bwd_kernel" and v["ScratchSize"]:
-            assert "Li1024ELi2E" in k, k
     assert seen == set(FAMILIES)
 
 
