@@ -110,7 +110,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_bwd_kernel(La
   __shared__ float2 red[2][TPR > 64 ? TPR / 64 : 1];
   __shared__ __align__(16) float share[RPB > 1 ? 2 * RPB * TPR * CH * N : 4];   // dw, then db: the rows' groups' sums, in the order of columns
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  constexpr bool AHEAD = CH * N <= 16 && TPR < 1024;   // (registers)
+  constexpr bool AHEAD = CH * N <= 16;   // (registers)
   constexpr bool KEEP = CH * N <= 16;   // the weights stay in registers; else they come from the caches, twice a row
   float w[CH][N], aw[CH][N], ab[CH][N];
 #pragma unroll
@@ -337,7 +337,7 @@ struct Split {
   // backward: so many elements of a row do not fit the registers beside their columns' sums, which are then formed in a pass of their
   // own (8192 rows of 16384 bf16 features: 370 us with the sums in scratch memory, 279 so)
   template <typename T>
-  static constexpr bool apart = TPR == 0 || TPR > 512 || CH * Piece<T>::N > 16;
+  static constexpr bool apart = TPR == 0 || CH * Piece<T>::N > 16 || (TPR > 512 && CH > 1);
 };
 // Calls f(Split) for the lanes and pieces of a row of `width`, f(Split<0, 0>) where no split holds it or it is less than a piece.
 template <typename T, bool BWD, typename F>
@@ -354,6 +354,8 @@ auto split_of(int32_t width, F f) {
   if constexpr (BWD && sizeof(T) == 2)
     if (pieces <= 256) return f(Split<256, 1>{});
   if (pieces <= 512) return f(Split<256, 2>{});
+  if constexpr (BWD && sizeof(T) == 2)   // 5120 features: 204 us with two pieces on 512 lanes, 170 so
+    if (pieces <= 1024) return f(Split<1024, 1>{});
   if (pieces <= 1024) return f(Split<512, 2>{});
   if (pieces <= 2048) return f(Split<512, 4>{});
   if constexpr (sizeof(T) == 4)
@@ -368,7 +370,16 @@ int64_t groups(int64_t rows, int units, int most) {
   const int64_t fit = (int64_t)units * (TPR > 256 ? 2 : most);
   return need < 1 ? 1 : need < fit ? need : fit;   // no rows: one, which sets the gradients to 0
 }
-constexpr int kFwdPerUnit = 8, kBwdPerUnit = 2;
+constexpr int kFwdPerUnit = 8;
+// Backward, workgroups per unit: two where the lanes have work, more where many of them lie behind the row's end and the loads under way are
+// fewer for it (256 MiB a tensor: 2048 bf16 features 145 us with two, 151 with three; 768: 158, 151; 320: 194, 164, with four 150).  fp32 rows
+// on four pieces a lane have room for two (768: 155, with three 173).
+template <typename T, typename S>
+int bwd_per_unit(int32_t width) {
+  const int pieces = (width + Piece<T>::N - 1) / Piece<T>::N, lanes = S::tpr * S::ch;
+  if (S::ch == 1 && pieces * 20 <= lanes * 13) return 4;
+  return pieces * 5 <= lanes * 4 && (sizeof(T) == 2 || S::ch < 4) ? 3 : 2;
+}
 
 template <typename S, typename K>
 void launch_rows(const LayerNormParams& p, int units, int most, hipStream_t s, K fits, K whole, K ragged, int piece) {
@@ -394,7 +405,7 @@ int64_t partials(int64_t rows, int32_t width, int units) {
   return split_of<T, true>(width, [&](auto split) -> int64_t {
     using S = decltype(split);
     if constexpr (S::template apart<T>) return rows < 1 ? 1 : rows < 64 * kWideRows ? (rows + kWideRows - 1) / kWideRows : 64;
-    const int64_t g = groups<S::tpr == 0 ? 64 : S::tpr>(rows, units, kBwdPerUnit);
+    const int64_t g = groups<S::tpr == 0 ? 64 : S::tpr>(rows, units, bwd_per_unit<T, S>(width));
     return g > 1 ? g : 0;
   });
 }
@@ -412,7 +423,7 @@ hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
     if constexpr (S::tpr == 0)
       hipLaunchKernelGGL(layer_norm_wide_bwd_kernel<T>, dim3((unsigned)groups<kWideThreads>(p.rows, units, 1)), dim3(kWideThreads), 0, s, p);
     else
-      launch_rows<S>(p, units, kBwdPerUnit, s, layer_norm_bwd_kernel<T, S::tpr, S::ch, kFits, !APART>,
+      launch_rows<S>(p, units, bwd_per_unit<T, S>(p.width), s, layer_norm_bwd_kernel<T, S::tpr, S::ch, kFits, !APART>,
                      layer_norm_bwd_kernel<T, S::tpr, S::ch, kWhole, !APART>, layer_norm_bwd_kernel<T, S::tpr, S::ch, kRagged, !APART>, Piece<T>::N);
     return hipGetLastError();
   });
