@@ -2,7 +2,7 @@
 //
 //   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum_rows dz
 //
-// Many rows: the tiled product (la2_linear_tiles.h), forward with its epilogue, backward twice.  A product whose tiles do not fill the
+// Many rows: the tiled product (la2_linear_tiles.h), forward with its epilogue, backward both in one launch.  A product whose tiles do not fill the
 // device is cut along the reduction; the pieces' fp32 sums meet in the workspace and are joined in a fixed order by a
 // launch of its own.  The backward pass forms dz (rounded to the operands' type, as the matrix instructions take it) and the bias'
 // gradient (from the unrounded values, fp32) in one pass over dy and z.

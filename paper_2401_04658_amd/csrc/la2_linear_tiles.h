@@ -1,7 +1,7 @@
 // The tiled matrix product (gfx950): one workgroup per TI x TJ tile of c (and piece of the reduction).
 //
 // Tiles of both operands stream from HBM straight into LDS (buffer loads with the LDS destination, 16 bytes per lane, no registers),
-// one reduction step of 128 bytes a row ahead of the one being multiplied; a buffer descriptor of its own per step bounds them, so
+// one reduction step of 128 bytes a row (the 64 tile: two or three) ahead of the one being multiplied; a buffer descriptor of its own per step bounds them, so
 // that rows behind a matrix' last one and elements behind the reduction's end arrive as 0.  One barrier per step.
 //
 // A wave owns (TI / WI) x (TJ / WJ) of the tile as 32 x 32 accumulators.  j is the accumulators' row index and i their column (a lane holds four
@@ -51,9 +51,11 @@ __device__ __forceinline__ f32x16 multiply<float>(const Frag<float>& a, const Fr
   return c;
 }
 
-// Direct load, 16 bytes per lane: LDS address lds + 16 lane, 0 for what lies outside the descriptor.
+// Direct load, 16 bytes per lane: LDS address lds + 16 lane, 0 for what lies outside the descriptor.  The compiler does not look into an asm
+// statement for the wait states between a vector instruction that writes a scalar register (a readfirstlane of the descriptor) and a memory
+// instruction that reads it, five; the statement brings them.
 __device__ __forceinline__ void load_lds(i32x4 rsrc, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :
                : "v"(off), "s"(rsrc), "s"(lds)
                : "m0", "memory");
