@@ -210,3 +210,23 @@ def test_search_as_a_program_runs_it():
     for n in range(3):
         step(again, torch.tensor([[said[b][i][n] for i in range(beams)] for b in range(batch)], device="cuda"))
     assert torch.equal(again, kv)
+
+
+def test_states_beyond_32_bits():
+    """128 beams of 36 MiB: a state buffer of more than 4 GiB; and logits of more."""
+    batch, beams, floats = 4, 32, 9 << 20
+    s = torch.empty(batch * beams, floats, device="cuda").normal_()
+    parent = torch.randint(0, beams, (batch, beams), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    rows = (parent.long() + beams * torch.arange(batch)[:, None]).reshape(-1).cuda()
+    want = s.view(batch * beams, -1, 4096)[:, ::97].index_select(0, rows)
+    la2.la2_beam_reorder(s, parent.cuda())
+    assert torch.equal(s.view(batch * beams, -1, 4096)[:, ::97], want)
+    del s, want
+    batch, beams, vocab = 1100, 8, 262144
+    logits = torch.empty(batch, beams, vocab, dtype=torch.bfloat16, device="cuda").normal_()
+    scores = torch.zeros(batch, beams, device="cuda")
+    got = la2.la2_beam_select(logits, scores)
+    tail = la2.la2_beam_select(logits[-3:], scores[-3:])
+    assert all(torch.equal(a[-3:], b) for a, b in zip(got[1:], tail[1:]))
+    # the rows alone are cut otherwise than the whole batch: sums of exp in another order, 2^-20
+    assert float((got[0][-3:] - tail[0]).abs().max()) <= 2 ** -19

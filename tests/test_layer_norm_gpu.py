@@ -168,3 +168,19 @@ def test_same_bits_in_every_run_in_place_and_on_another_stream():
         want = la2.la2_layer_norm_bwd(dy, x, mean, rstd, w)
         got = la2.la2_layer_norm_bwd(dy, x, mean, rstd, w, out=dy)
         assert got[0] is not None and all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+def test_offsets_beyond_32_bits():
+    rows, width, last = (1 << 32) // (2 * 2048) + 700, 2048, 1000   # 4 GiB and a little more a tensor
+    x = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda").normal_()
+    w, b = torch.randn(width, device="cuda"), torch.randn(width, device="cuda")
+    y, mean, rstd = la2.la2_layer_norm_fwd(x, w, b)
+    tail = la2.la2_layer_norm_fwd(x[-last:], w, b)
+    assert torch.equal(y[-last:], tail[0]) and torch.equal(mean[-last:], tail[1]) and torch.equal(rstd[-last:], tail[2])
+    dx, dw, db = la2.la2_layer_norm_bwd(y, x, mean, rstd, w)
+    assert torch.equal(dx[-last:], la2.la2_layer_norm_bwd(y[-last:], x[-last:], mean[-last:], rstd[-last:], w)[0])
+    # the sums over a million rows, in 64 bits a part at a time; a million terms in fp32 are off by a million roundings at most, in fact by far
+    # fewer: rows are summed by 512 workgroups of 256 lanes first
+    want = sum(p.double().sum(0) for p in y.split(1 << 16))
+    mag = sum(p.abs().sum(0, dtype=torch.float64) for p in y.split(1 << 16))
+    assert bool(((db.double() - want).abs() <= (rows / 512 + 520) * ref.U32 * mag).all())

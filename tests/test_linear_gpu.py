@@ -202,3 +202,15 @@ def test_same_bits_in_every_run_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(want, out))
         step()
+
+
+def test_offsets_beyond_32_bits():
+    rows, k, n, last = (1 << 32) // (2 * 2048) + 300, 2048, 72, 500   # x, and dx, of 4 GiB and a little more
+    x = torch.empty(rows, k, dtype=torch.bfloat16, device="cuda").normal_()
+    w = torch.randn(n, k, device="cuda").mul_(0.02).bfloat16()
+    y, _ = la2.la2_linear_fwd(x, w)
+    ry, ey, _, _ = ref.linear_fwd(x[-last:], w, None, None, "none")
+    ref.within("y", y[-last:], ry, ey)
+    dx, _, _ = la2.la2_linear_bwd(y, x, w, want_dw=False)
+    rdx, edx = ref.linear_bwd(y[-last:], x[-last:], w, None, "none")[:2]
+    ref.within("dx", dx[-last:], rdx, edx)
