@@ -14,7 +14,7 @@
 //           transposing read of 32 lanes (4 rows, 64 bytes of each) meets all banks once.  fp32: in place, lanes read consecutive elements.
 //
 // Bound by the matrix pipes and LDS together (a step of the 256 tile keeps each busy for 2048 cycles of about 3000).  16384 x 8192 x 2048 bf16: the
-// weight's gradient 436 us (1.26 PFLOP/s), the input's 469, forward 490 and with gelu and kept sums 560; 8192 x 8192 x 8192 1.2 PFLOP/s.  fp32
+// weight's gradient 436 us (1.26 PFLOP/s), the input's 469, forward 490 and with gelu and kept sums 564; 8192 x 8192 x 8192 1.2 PFLOP/s.  fp32
 // 4096 x 4096 x 4096: 142 TFLOP/s, the rate of the fp32 matrix instructions.
 #ifndef LA2_LINEAR_TILES_H_
 #define LA2_LINEAR_TILES_H_
