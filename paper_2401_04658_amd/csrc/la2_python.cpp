@@ -308,16 +308,19 @@ Rows rows_of(const at::Tensor& t, const char* what) {
   }
   r.width = t.size(dims - 1);
   r.stride = r.width;
-  int64_t next = 0;   // stride that the dimension in front of those seen has to have; 0: any
+  for (int64_t d = 0; d < dims - 1; d++) r.rows *= t.size(d);
+  if (t.numel() == 0) return r;   // no element, no distance
+  bool seen = false;   // a dimension of more than one entry, and with it the rows' distance
+  int64_t next = 0;    // stride that the dimension in front of those seen has to have
   for (int64_t d = dims - 2; d >= 0; d--) {
     const int64_t n = t.size(d);
-    r.rows *= n;
     if (n == 1) continue;
-    if (next == 0) r.stride = t.stride(d);
+    if (!seen) r.stride = t.stride(d);
     else if (t.stride(d) != next) {
       PyErr_Format(PyExc_ValueError, "la2: %s must be rows at one distance", what);
       throw Raised{};
     }
+    seen = true;
     next = t.stride(d) * n;
   }
   return r;

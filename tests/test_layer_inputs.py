@@ -1,0 +1,96 @@
+"""Which tensors the binding of the operators around the recurrence takes and which it refuses (host code only; nothing is launched)."""
+import pytest
+import torch
+
+from paper_2401_04658_amd import binding
+
+ALIGN, LAUNCH = 4, 6
+
+
+@pytest.fixture
+def entries(monkeypatch):
+    """The binding's functions on CPU tensors; a call that passes every check ends with LA2_ERR_LAUNCH, there being no device."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that passes the checks would launch")
+    monkeypatch.setattr(binding, "_on_gpu", lambda t, what: None)
+    monkeypatch.setattr(binding, "_call", lambda entry, t, *args: entry(*args, 0))
+    return binding
+
+
+def zeros(*size, dtype=torch.bfloat16):
+    return torch.zeros(size, dtype=dtype)
+
+
+def scratch(size=1 << 20):
+    """A workspace at a multiple of 256, as device memory is and host memory is not always."""
+    t = torch.empty(size + 256, dtype=torch.uint8)
+    skip = -t.data_ptr() % 256
+    return t[skip:skip + size]
+
+
+def calls(la2, t):
+    """Every entry point that takes t [a, b, 128] as rows of features, t in each of the places where it does."""
+    lead, dense, w, ws = t.shape[:-1], zeros(*t.shape), zeros(128, 128), scratch()
+    stats = zeros(*lead, dtype=torch.float32)
+    return {
+        "layer_norm_fwd x": lambda: la2.la2_layer_norm_fwd(t),
+        "layer_norm_bwd x, dy": lambda: la2.la2_layer_norm_bwd(t, t, stats, stats, workspace=ws),
+        "linear_fwd x": lambda: la2.la2_linear_fwd(t, w),
+        "linear_fwd residual": lambda: la2.la2_linear_fwd(dense, w, residual=t),
+        "linear_fwd out": lambda: la2.la2_linear_fwd(dense, w, out=t),
+        "linear_bwd x": lambda: la2.la2_linear_bwd(dense, t, w, workspace=ws),
+        "linear_bwd dy": lambda: la2.la2_linear_bwd(t, dense, w, workspace=ws),
+        "beam_select logits": lambda: la2.la2_beam_select(t, stats, workspace=ws),
+    }
+
+
+EXPANDED = [  # size before expand(3, 4, 128)
+    (3, 1, 128),    # the middle: a gradient per sequence for all its positions, logits of a prompt for all its beams
+    (1, 4, 128),    # the leading dimension
+    (1, 1, 128),    # both
+]
+
+
+@pytest.mark.parametrize("size", EXPANDED)
+def test_rows_that_share_memory_are_refused(entries, size):
+    t = zeros(*size).expand(3, 4, 128)
+    for name, call in calls(entries, t).items():
+        try:
+            got = call()
+        except ValueError:
+            continue
+        assert got == ALIGN, name
+
+
+def test_more_leading_dimensions(entries):
+    for size, full in (((2, 3, 1, 64), (2, 3, 4, 64)), ((2, 1, 4, 64), (2, 3, 4, 64)), ((1, 3, 4, 64), (2, 3, 4, 64)), ((2, 1, 1, 64), (2, 3, 4, 64)),
+                       ((1, 64), (4, 64)), ((1, 1, 64), (4, 1, 64))):
+        t = zeros(*size).expand(*full)
+        try:
+            got = entries.la2_layer_norm_fwd(t)
+        except ValueError:
+            continue
+        assert got == ALIGN, size
+    # overlapping rather than expanded
+    for stride in ((64, 64, 1), (128, 64, 1), (96, 96, 1)):
+        with pytest.raises(ValueError):
+            entries.la2_layer_norm_fwd(zeros(2000).as_strided((3, 4, 64), stride))
+    assert entries.la2_layer_norm_fwd(zeros(2000).as_strided((3, 4, 64), (128, 32, 1))) == ALIGN
+
+
+def test_rows_at_one_distance_are_taken(entries):
+    wide = zeros(6, 4, 192)
+    for t in (zeros(3, 4, 128), zeros(12, 160)[:, :128].view(3, 4, 128), wide[::2, :, :128][:, :1], wide[:3, :1, :128], wide[:1, ::2, :128],
+              zeros(3, 1, 128), zeros(1, 1, 128), zeros(1, 1, 128).expand(1, 1, 128), zeros(3, 128).unsqueeze(1)):
+        for name, call in calls(entries, t).items():
+            assert call() == LAUNCH, (name, t.shape, t.stride())
+
+
+def test_no_rows_at_any_distance(entries):
+    """Tensors without elements: whatever their strides say, as torch leaves them behind slicing."""
+    for t in (zeros(3, 0, 128), zeros(0, 4, 128), zeros(3, 4, 128)[:, :0], zeros(3, 4, 192)[:0, :, :128], zeros(3, 8, 192)[:, 4:4, :128]):
+        stats = zeros(*t.shape[:-1], dtype=torch.float32)
+        assert entries.la2_layer_norm_fwd(t)[0].shape == t.shape
+        assert entries.la2_linear_fwd(t, zeros(64, 128))[0].shape == t.shape[:-1] + (64,)
+        assert entries.la2_layer_norm_bwd(t, t, stats, stats, want_d_weight=False, want_d_bias=False)[0].shape == t.shape
+        assert entries.la2_linear_bwd(t, t, zeros(128, 128), want_dw=False, want_d_bias=False)[0].shape == t.shape
