@@ -388,11 +388,14 @@ PyObject* answer(la2_status st, const T&... t) {
   Py_DECREF(out);
   return nullptr;
 }
-template <typename F>
-la2_status unlocked(F f) {
+// The call without the interpreter lock.  Its arguments are evaluated before the lock is released: what can raise (a pointer of a
+// tensor without storage, an extent) raises with the lock held.
+template <typename... P, typename... A>
+la2_status unlocked(la2_status (*entry)(P...), A... args) {
+  static_assert(sizeof...(P) == sizeof...(A), "the entry point's arguments");
   la2_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = f();
+  st = entry(args...);
   Py_END_ALLOW_THREADS
   return st;
 }
@@ -421,10 +424,9 @@ PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor y = same_or_new(a[4], x, "out"), mean = dense_or_new(a[5], x, at::kFloat, lead, "mean"),
                      rstd = dense_or_new(a[6], x, at::kFloat, lead, "rstd");
     void* const stream = Arg<void*>(a[7]).get();
-    return answer(unlocked([&] {
-      return la2_layer_norm_fwd(r.rows, extent(r.width), dtype, r.stride, x.data_ptr(), weight, bias, eps, y.data_ptr(),
-                                static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), stream);
-    }), y, mean, rstd);
+    return answer(unlocked(la2_layer_norm_fwd, r.rows, extent(r.width), dtype, r.stride, x.data_ptr(), weight, bias, eps, y.data_ptr(),
+                           static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), stream),
+                  y, mean, rstd);
   });
 }
 
@@ -447,10 +449,9 @@ PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t width = extent(r.width);
     const at::Tensor ws = workspace_of(a[8], x, dw.defined() || db.defined() ? la2_layer_norm_workspace_bytes(r.rows, width, dtype) : 0);
     void* const stream = Arg<void*>(a[9]).get();
-    return answer(unlocked([&] {
-      return la2_layer_norm_bwd(r.rows, width, dtype, r.stride, x.data_ptr(), dy.data_ptr(), weight, mean, rstd, dx.data_ptr(),
-                                static_cast<float*>(data(dw)), static_cast<float*>(data(db)), data(ws), bytes(ws), stream);
-    }), dx, dw, db);
+    return answer(unlocked(la2_layer_norm_bwd, r.rows, width, dtype, r.stride, x.data_ptr(), dy.data_ptr(), weight, mean, rstd,
+                           dx.data_ptr(), static_cast<float*>(data(dw)), static_cast<float*>(data(db)), data(ws), bytes(ws), stream),
+                  dx, dw, db);
   });
 }
 
@@ -501,9 +502,9 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[7] != Py_None || truth(a[5])) pre = same_or_new(a[7], y, "pre");
     const at::Tensor ws = workspace_of(a[8], x, la2_linear_workspace_bytes(&d, LA2_OP_FWD));
     void* const stream = Arg<void*>(a[9]).get();
-    return answer(unlocked([&] {
-      return la2_linear_fwd(&d, x.data_ptr(), w.data_ptr(), bias, residual, y.data_ptr(), data(pre), data(ws), bytes(ws), stream);
-    }), y, pre);
+    return answer(unlocked(la2_linear_fwd, &d, x.data_ptr(), w.data_ptr(), bias, residual, y.data_ptr(), data(pre), data(ws), bytes(ws),
+                           stream),
+                  y, pre);
   });
 }
 
@@ -526,10 +527,9 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (truth(a[7])) db = fresh({d.out_features}, x, at::kFloat);
     const at::Tensor ws = workspace_of(a[8], x, la2_linear_workspace_bytes(&d, LA2_OP_BWD));
     void* const stream = Arg<void*>(a[9]).get();
-    return answer(unlocked([&] {
-      return la2_linear_bwd(&d, x.data_ptr(), w.data_ptr(), pre, dy.data_ptr(), data(dx), data(dw), static_cast<float*>(data(db)), data(ws),
-                            bytes(ws), stream);
-    }), dx, dw, db);
+    return answer(unlocked(la2_linear_bwd, &d, x.data_ptr(), w.data_ptr(), pre, dy.data_ptr(), data(dx), data(dw), static_cast<float*>(data(db)),
+                           data(ws), bytes(ws), stream),
+                  dx, dw, db);
   });
 }
 
@@ -550,11 +550,10 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor out = fresh(lead, logits, at::kFloat), parent = fresh(lead, logits, at::kInt), token = fresh(lead, logits, at::kInt),
                      done = fresh(lead, logits, at::kBool);
     void* const stream = Arg<void*>(a[5]).get();
-    return answer(unlocked([&] {
-      return la2_beam_select(batch, beams, vocab, dtype, r.stride, logits.data_ptr(), scores, finished, eos, static_cast<float*>(out.data_ptr()),
-                             static_cast<int32_t*>(parent.data_ptr()), static_cast<int32_t*>(token.data_ptr()),
-                             static_cast<uint8_t*>(done.data_ptr()), data(ws), bytes(ws), stream);
-    }), out, parent, token, done);
+    return answer(unlocked(la2_beam_select, batch, beams, vocab, dtype, r.stride, logits.data_ptr(), scores, finished, eos,
+                           static_cast<float*>(out.data_ptr()), static_cast<int32_t*>(parent.data_ptr()),
+                           static_cast<int32_t*>(token.data_ptr()), static_cast<uint8_t*>(done.data_ptr()), data(ws), bytes(ws), stream),
+                  out, parent, token, done);
   });
 }
 
@@ -587,7 +586,7 @@ PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* const stream = Arg<void*>(a[2]).get();
     const int32_t states = extent(count);
     const int32_t* const from = static_cast<const int32_t*>(parent.data_ptr());
-    return PyLong_FromLong((long)unlocked([&] { return la2_beam_reorder(states, at.data(), batch, beams, row, from, stream); }));
+    return PyLong_FromLong((long)unlocked(la2_beam_reorder, states, at.data(), batch, beams, row, from, stream));
   });
 }
 

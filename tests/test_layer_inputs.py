@@ -94,3 +94,28 @@ def test_no_rows_at_any_distance(entries):
         assert entries.la2_linear_fwd(t, zeros(64, 128))[0].shape == t.shape[:-1] + (64,)
         assert entries.la2_layer_norm_bwd(t, t, stats, stats, want_d_weight=False, want_d_bias=False)[0].shape == t.shape
         assert entries.la2_linear_bwd(t, t, zeros(128, 128), want_dw=False, want_d_bias=False)[0].shape == t.shape
+
+
+def test_an_extent_that_does_not_fit_raises():
+    x = torch.empty(0, 2 ** 31, dtype=torch.bfloat16)
+    v = torch.empty(0)
+    lib = binding._module()
+    for call in (lambda: lib.layer_norm_fwd(x, None, None, 1e-5, None, None, None, 0),
+                 lambda: lib.layer_norm_bwd(x, x, v, v, None, False, False, None, None, 0),
+                 lambda: lib.linear_fwd(x, x, None, None, 0, False, None, None, None, 0)):
+        with pytest.raises(OverflowError):
+            call()
+
+
+def test_tensors_without_storage_raise():
+    """What torch.func hands to a function it transforms has sizes and strides but no memory: an error, with the interpreter lock held."""
+    lib, x, w, square = binding._module(), zeros(2, 4, 64), zeros(2, 32, 64), zeros(2, 64, 64)
+    v, scores, parent = torch.zeros(4), torch.zeros(2, 2), torch.zeros(2, 2, dtype=torch.int32)
+    for call in (lambda: torch.func.vmap(lambda t: lib.layer_norm_fwd(t, None, None, 1e-5, None, None, None, 0))(x),
+                 lambda: torch.func.vmap(lambda t: lib.layer_norm_bwd(x[0], t, v, v, None, False, False, None, None, 0), randomness="same")(x),
+                 lambda: torch.func.vmap(lambda t, u: lib.linear_fwd(t, u, None, None, 0, False, None, None, None, 0))(x, w),
+                 lambda: torch.func.vmap(lambda t, u: lib.linear_bwd(t, t, u, None, 0, True, True, True, None, 0))(x, square),
+                 lambda: torch.func.vmap(lambda t: lib.beam_select(t, scores, None, -1, None, 0))(torch.zeros(2, 2, 2, 9)),
+                 lambda: torch.func.vmap(lambda t: lib.beam_reorder([t], parent, 0))(torch.zeros(2, 4, 8))):
+        with pytest.raises(RuntimeError, match="data pointer"):
+            call()
