@@ -495,8 +495,8 @@ typedef struct {
 } la2_linear_desc;
 
 /*
- * Bytes of workspace of la2_linear_fwd (op LA2_OP_FWD) or la2_linear_bwd (LA2_OP_BWD, all outputs wanted); 0 for an invalid
- * descriptor.  It holds copies of operands whose rows are no whole 16-byte pieces, the sums of products whose reduction is cut,
+ * Bytes of workspace of la2_linear_fwd (op LA2_OP_FWD) or la2_linear_bwd (LA2_OP_BWD), enough whichever of its outputs are wanted;
+ * 0 for an invalid descriptor.  It holds copies of operands whose rows are no whole 16-byte pieces, the sums of products whose reduction is cut,
  * dz, and the rows' shares of d_bias.  Depends on the device's compute-unit count.  256-byte aligned; may be NULL when 0.
  */
 size_t la2_linear_workspace_bytes(const la2_linear_desc* desc, int32_t op);
@@ -512,7 +512,8 @@ la2_status la2_linear_fwd(const la2_linear_desc* desc, const void* x, const void
                           void* hip_stream);
 /*
  *   pre       z as the forward pass left it; may be NULL for LA2_ACT_NONE
- *   dx, dw, d_bias  out, NULL where not wanted (x is then not needed for dw, w not for dx)
+ *   dx, dw, d_bias  out, NULL where not wanted (x is read for dw alone, w for dx alone).  How a reduction is cut, and so the last bits of
+ *             a result, may depend on which of dx and dw are wanted together
  * dz is rounded to dtype for the two products (16-bit data), d_bias is formed from the unrounded values.  No rows: dw and d_bias are 0.
  */
 la2_status la2_linear_bwd(const la2_linear_desc* desc, const void* x, const void* w, const void* pre,

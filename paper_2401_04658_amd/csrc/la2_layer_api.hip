@@ -138,9 +138,19 @@ size_t la2_linear_workspace_bytes(const la2_linear_desc* desc, int32_t op) {
   la2::LinearParams p = linear_params(desc);
   if (op == LA2_OP_FWD) return la2::linear_fwd_workspace(p, la2::device_units());
   if (op != LA2_OP_BWD) return 0;
+  // Each choice of outputs has a plan of its own, and one product alone may be cut into more pieces than beside the other: the largest
+  // need (d_bias only adds to it).
   static float wanted;   // only told from nullptr
-  p.dx = p.dw = p.d_bias = &wanted;
-  return la2::linear_bwd_workspace(p, la2::device_units());
+  const int units = la2::device_units();
+  p.d_bias = &wanted;
+  size_t most = 0;
+  for (int products = 1; products <= 3; products++) {
+    p.dx = products & 1 ? &wanted : nullptr;
+    p.dw = products & 2 ? &wanted : nullptr;
+    const size_t need = la2::linear_bwd_workspace(p, units);
+    most = need > most ? need : most;
+  }
+  return most;
 }
 
 la2_status la2_linear_fwd(const la2_linear_desc* desc, const void* x, const void* w, const float* bias, const void* residual, void* y,
