@@ -361,8 +361,10 @@ const T* dense_or_null(PyObject* o, const at::Tensor& ref, at::ScalarType type, 
 // The caller's workspace or a new one of `need` bytes (undefined for none)
 at::Tensor workspace_of(PyObject* o, const at::Tensor& ref, size_t need) {
   if (o != Py_None) {
-    if (tensor(o).device() != ref.device()) raise(PyExc_ValueError, "la2: the workspace is on another device");
-    return tensor(o);
+    const at::Tensor& t = tensor(o);
+    if (t.device() != ref.device()) raise(PyExc_ValueError, "la2: the workspace is on another device");
+    if (!t.is_contiguous()) raise(PyExc_ValueError, "la2: the workspace must be contiguous");   // its bytes are counted from its elements
+    return t;
   }
   return need == 0 ? at::Tensor() : fresh({(int64_t)need}, ref, at::kByte);
 }

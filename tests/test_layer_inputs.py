@@ -119,3 +119,14 @@ def test_tensors_without_storage_raise():
                  lambda: torch.func.vmap(lambda t: lib.beam_reorder([t], parent, 0))(torch.zeros(2, 4, 8))):
         with pytest.raises(RuntimeError, match="data pointer"):
             call()
+
+
+def test_a_workspace_without_its_bytes_is_refused(entries):
+    """One byte expanded to many counts as many and has one."""
+    x, w, v = zeros(300, 128), zeros(64, 128), torch.zeros(300)
+    dy, logits, scores = zeros(300, 64), zeros(2, 2, 9), torch.zeros(2, 2)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 30), torch.zeros(1, 1 << 10).expand(1 << 10, 1 << 10), scratch()[::2]):
+        for call in (lambda: entries.la2_layer_norm_bwd(x, x, v, v, workspace=ws), lambda: entries.la2_linear_fwd(x, w, workspace=ws),
+                     lambda: entries.la2_linear_bwd(dy, x, w, workspace=ws), lambda: entries.la2_beam_select(logits, scores, workspace=ws)):
+            with pytest.raises(ValueError):
+                call()
