@@ -325,8 +325,15 @@ Rows rows_of(const at::Tensor& t, const char* what) {
   }
   return r;
 }
+// The strides that elements lie at: those of dimensions of one entry count for nothing
+bool same_strides(const at::Tensor& t, const at::Tensor& ref) {
+  if (t.numel() == 0) return true;
+  for (int64_t d = 0; d < t.dim(); d++)
+    if (t.size(d) > 1 && t.stride(d) != ref.stride(d)) return false;
+  return true;
+}
 void same_rows(const at::Tensor& t, const at::Tensor& ref, const char* what) {
-  if (t.sizes() != ref.sizes() || t.strides() != ref.strides() || t.scalar_type() != ref.scalar_type() || t.device() != ref.device()) {
+  if (t.sizes() != ref.sizes() || !same_strides(t, ref) || t.scalar_type() != ref.scalar_type() || t.device() != ref.device()) {
     PyErr_Format(PyExc_ValueError, "la2: %s: another shape, layout, dtype or device than expected", what);
     throw Raised{};
   }

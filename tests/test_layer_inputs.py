@@ -130,3 +130,22 @@ def test_a_workspace_without_its_bytes_is_refused(entries):
                      lambda: entries.la2_linear_bwd(dy, x, w, workspace=ws), lambda: entries.la2_beam_select(logits, scores, workspace=ws)):
             with pytest.raises(ValueError):
                 call()
+
+
+def test_strides_of_dimensions_of_one_entry_do_not_count(entries):
+    """A step's [batch, 1, features] sliced out of a longer tensor lies as a dense one does."""
+    ws, v, w = scratch(), torch.zeros(1, 1), zeros(64, 64)
+    long = zeros(1, 7, 64)
+    one, dense = long[:, 3:4], zeros(1, 1, 64)
+    dense_b, part_b = zeros(5, 1, 64), zeros(5, 1, 64).as_strided((5, 1, 64), (64, 9, 1))
+    vb = torch.zeros(5, 1)
+    assert one.stride() != dense.stride() and part_b.stride() != dense_b.stride()
+    for a, b, s in ((one, dense, v), (dense, one, v), (part_b, dense_b, vb), (dense_b, part_b, vb)):
+        for call in (lambda: entries.la2_layer_norm_fwd(a, out=b), lambda: entries.la2_layer_norm_bwd(a, b, s, s, workspace=ws),
+                     lambda: entries.la2_linear_fwd(a, w, residual=a, out=b, pre=a.clone()),
+                     lambda: entries.la2_linear_bwd(a, b, w, pre=b, act="gelu", workspace=ws)):
+            assert call() == LAUNCH, (a.stride(), b.stride())
+    columns = zeros(4, 6).t()[:, :1]   # features of one entry: [6, 1], rows one element apart
+    assert entries.la2_layer_norm_fwd(columns, out=zeros(6, 1)) == LAUNCH
+    with pytest.raises(ValueError):
+        entries.la2_layer_norm_fwd(zeros(5, 1, 96)[:, :, :64], out=dense_b)
