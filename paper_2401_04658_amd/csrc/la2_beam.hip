@@ -291,7 +291,7 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
         score[k] = ordered((double)start[beam] + (((double)from_ordered((uint32_t)(key[k] >> 32)) - base[beam]) - log_sum[beam]));
         place[k] = ~((uint32_t)beam * (uint32_t)p.vocab + (0xFFFFFFFFu - (uint32_t)key[k]));
       } else if (kind[beam] == 2 && c == beam * per) {
-        score[k] = ordered((double)start[beam]);
+        score[k] = ordered((double)start[beam] + 0.0);   // (the two zeros are one)
         place[k] = ~((uint32_t)beam * (uint32_t)p.vocab + (uint32_t)p.eos);
       }
       if (score[k] > top || (score[k] == top && place[k] > top_place)) {
