@@ -504,7 +504,8 @@ size_t la2_linear_workspace_bytes(const la2_linear_desc* desc, int32_t op);
 /*
  *   bias      fp32 [out_features] or NULL;  residual  or NULL
  *   pre       out  z (rounded to dtype), for the backward pass, or NULL if not wanted
- * y may be residual.  Rows of at most 2^23 - 1 bytes, fewer than 2^31 of them, at most 2^40 elements per matrix (LA2_ERR_SHAPE).
+ * y may be residual.  Rows of at most 2^23 - 1 bytes, fewer than 2^31 of them, at most 2^40 elements per matrix, fewer than 2^23 - 2^18 tiles of
+ * 256 x 256 in y, and in dx and dw together, a part of a tile counting as one (LA2_ERR_SHAPE).
  * fp32 data: products and sums in fp32 (the fp32 matrix instructions).
  */
 la2_status la2_linear_fwd(const la2_linear_desc* desc, const void* x, const void* w, const float* bias,

@@ -39,18 +39,6 @@ size_t norm_workspace(int64_t rows, int32_t width, int32_t dtype) {
   return (size_t)la2::layer_norm_bwd_partials(dtype, rows, width, la2::device_units()) * 2 * width * sizeof(float);
 }
 
-la2_status check_linear(const la2_linear_desc* d) {
-  if (d == nullptr) return LA2_ERR_NULL;
-  if (!known_dtype(d->dtype)) return LA2_ERR_DTYPE;
-  if (d->rows < 0 || d->in_features < 0 || d->out_features < 0) return LA2_ERR_SHAPE;
-  if (d->act < LA2_ACT_NONE || d->act > LA2_ACT_SILU) return LA2_ERR_VALUE;
-  if (d->stride_x < d->in_features || d->stride_w < d->in_features || d->stride_y < d->out_features) return LA2_ERR_STRIDE_ALIGN;
-  // a tile's rows are addressed with 31-bit byte offsets, 256 rows at most
-  const int64_t most = (((int64_t)1 << 23) - 1) / (d->dtype == LA2_F32 ? 4 : 2);
-  if (d->stride_x > most || d->stride_w > most || d->stride_y > most) return LA2_ERR_SHAPE;
-  if (d->rows > INT32_MAX || d->rows > kMostElements / (1 + (d->in_features > d->out_features ? d->in_features : d->out_features))) return LA2_ERR_SHAPE;
-  return LA2_OK;
-}
 la2::LinearParams linear_params(const la2_linear_desc* d) {
   la2::LinearParams p{};
   p.rows = d->rows;
@@ -62,6 +50,18 @@ la2::LinearParams linear_params(const la2_linear_desc* d) {
   p.stride_w = d->stride_w;
   p.stride_y = d->stride_y;
   return p;
+}
+la2_status check_linear(const la2_linear_desc* d) {
+  if (d == nullptr) return LA2_ERR_NULL;
+  if (!known_dtype(d->dtype)) return LA2_ERR_DTYPE;
+  if (d->rows < 0 || d->in_features < 0 || d->out_features < 0) return LA2_ERR_SHAPE;
+  if (d->act < LA2_ACT_NONE || d->act > LA2_ACT_SILU) return LA2_ERR_VALUE;
+  if (d->stride_x < d->in_features || d->stride_w < d->in_features || d->stride_y < d->out_features) return LA2_ERR_STRIDE_ALIGN;
+  // a tile's rows are addressed with 31-bit byte offsets, 256 rows at most
+  const int64_t most = (((int64_t)1 << 23) - 1) / (d->dtype == LA2_F32 ? 4 : 2);
+  if (d->stride_x > most || d->stride_w > most || d->stride_y > most) return LA2_ERR_SHAPE;
+  if (d->rows > INT32_MAX || d->rows > kMostElements / (1 + (d->in_features > d->out_features ? d->in_features : d->out_features))) return LA2_ERR_SHAPE;
+  return la2::linear_fits(linear_params(d)) ? LA2_OK : LA2_ERR_SHAPE;
 }
 
 la2_status check_beams(int32_t batch, int32_t beams) {

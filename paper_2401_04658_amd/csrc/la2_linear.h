@@ -48,6 +48,9 @@ struct LinearParams {
   void *dx, *dw;
   float* d_bias;
 };
+// Whether the products' grids stay below the 2^32 work-items that a launch may have, with the largest tile: fewer than 2^23 workgroups of 512
+// threads, 2^18 of them set aside for those that sum d_bias.
+bool linear_fits(const LinearParams& p);
 size_t linear_fwd_workspace(const LinearParams& p, int units);
 size_t linear_bwd_workspace(const LinearParams& p, int units);
 hipError_t launch_linear_fwd(const LinearParams& p, void* workspace, int units, hipStream_t s);
@@ -65,6 +68,9 @@ struct PairParams {
 };
 
 enum { kTile64 = 0, kTile128 = 1, kTile256 = 2, kTiles = 3 };
+constexpr int kTileThreads[kTiles] = {256, 256, 512};
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1;   // of a grid
+constexpr int64_t kMostSumGroups = 1 << 18;                // workgroups that sum d_bias: 16 columns each, rows of less than 2^23 bytes
 hipError_t launch_product_bf16(int tile, const ProductParams& p, hipStream_t s);
 hipError_t launch_product_f16(int tile, const ProductParams& p, hipStream_t s);
 hipError_t launch_product_f32(int tile, const ProductParams& p, hipStream_t s);

@@ -276,6 +276,7 @@ Plan plan_products(int dtype, const Extent* e, int count, int units) {
         }
       }
       if (cut > 0 && (!cuts || sums > 512e6)) continue;
+      if ((groups + kMostSumGroups) * kTileThreads[tile] > kMostThreads) continue;   // (the 256 tile, not cut, always stays: linear_fits)
       const double share = work / units;
       if (groups <= units) time += longest;
       else if (count == 1) time += std::max(longest, std::ceil((double)groups / units) * shortest);
@@ -462,6 +463,12 @@ hipError_t backward(const LinearParams& q, Taker& t, bool count_only, int units,
 }
 
 }  // namespace
+
+bool linear_fits(const LinearParams& p) {
+  const int64_t T = 64 << kTile256, rows = (p.rows + T - 1) / T, in = (p.in + T - 1) / T, out = (p.out + T - 1) / T;
+  const int64_t most = kMostThreads / kTileThreads[kTile256] - kMostSumGroups;
+  return rows * out <= most && rows * in + out * in <= most;
+}
 
 size_t linear_fwd_workspace(const LinearParams& p, int units) {
   Taker t{nullptr};

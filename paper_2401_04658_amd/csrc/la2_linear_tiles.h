@@ -184,6 +184,7 @@ template <int TI_, int TJ_, int WI_, int WJ_, int STAGES_>
 struct Shape {
   static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, STAGES = STAGES_, NW = WI * WJ, THREADS = 64 * NW;
   static constexpr int BYTES = (TI + TJ) * kStepBytes * STAGES;
+  static_assert(TI == TJ && THREADS == kTileThreads[TI / 128], "as planned");
 };
 
 // Workgroup `wg` of the tiles of p
