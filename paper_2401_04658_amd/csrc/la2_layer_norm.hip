@@ -433,13 +433,14 @@ hipError_t bwd(const LayerNormParams& p, int units, hipStream_t s) {
 
 }  // namespace
 
-// 16 columns a workgroup, 64 threads each
+// 16 columns a workgroup, 64 threads each; `from`: the launch's first column
 constexpr int kSumCols = 16, kSumSlices = 64;
+constexpr int64_t kSumMost = 1 << 25;   // columns of a launch: a grid has at most 2^32 - 1 work-items
 __global__ __launch_bounds__(kSumCols * kSumSlices) void column_sum_kernel(const float* partial, int64_t count, int64_t columns, int64_t first,
-                                                                           float* a, float* b) {
+                                                                           int64_t from, float* a, float* b) {
   __shared__ float part[kSumSlices][kSumCols + 1];
   const int col = threadIdx.x % kSumCols, slice = threadIdx.x / kSumCols;
-  const int64_t j = (int64_t)blockIdx.x * kSumCols + col;
+  const int64_t j = from + (int64_t)blockIdx.x * kSumCols + col;
   float v = 0.f;
   if (j < columns) {
 #pragma unroll 8
@@ -458,9 +459,14 @@ __global__ __launch_bounds__(kSumCols * kSumSlices) void column_sum_kernel(const
   }
 }
 hipError_t launch_column_sums(const float* partial, int64_t count, int64_t columns, int64_t first, float* a, float* b, hipStream_t s) {
-  hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((columns + kSumCols - 1) / kSumCols)), dim3(kSumCols * kSumSlices), 0, s, partial, count,
-                     columns, first, a, b);
-  return hipGetLastError();
+  for (int64_t from = 0; from < columns; from += kSumMost) {
+    const int64_t n = columns - from < kSumMost ? columns - from : kSumMost;
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), dim3(kSumCols * kSumSlices), 0, s, partial, count, columns,
+                       first, from, a, b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_layer_norm_fwd(int dtype, const LayerNormParams& p, int units, hipStream_t s) {
