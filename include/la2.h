@@ -547,7 +547,7 @@ la2_status la2_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t 
  * decode states, say), each dense [batch, beams, row_bytes], as one launch per 64 of them.
  *   states    HOST array of nstates device pointers, 16-byte aligned;  row_bytes  a multiple of 16 (LA2_ERR_STRIDE_ALIGN)
  *   parent    int32 [batch, beams]; a value outside 0 .. beams - 1 leaves its beam as it is
- * 1 <= beams <= 32, batch <= 65535 (LA2_ERR_SHAPE).  A beam that is its own parent is neither read nor written.
+ * 1 <= beams <= 32, batch <= 65535, row_bytes <= 2^36 - 4096 (LA2_ERR_SHAPE).  A beam that is its own parent is neither read nor written.
  */
 la2_status la2_beam_reorder(int32_t nstates, void* const* states, int32_t batch, int32_t beams, int64_t row_bytes,
                             const int32_t* parent, void* hip_stream);

@@ -346,7 +346,6 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamSelectParams p)
 // change in place whatever the parents are.  Sources that several beams take come from the caches after the first read; a beam that
 // is its own parent is not touched: its buffer descriptor is empty, which keeps the loads and stores free of branches and
 // all of them in flight.  Bound by memory: 2 x 128 states of 2 MiB, 7 in 8 of them moving, 153 us (5.2 TB/s).
-constexpr int kReorderThreads = 256;
 template <int MAX>
 __global__ __launch_bounds__(kReorderThreads) void beam_reorder_kernel(BeamReorderParams p) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -419,11 +418,11 @@ hipError_t launch_beam_select(int dtype, BeamSelectParams p, int units, hipStrea
 
 hipError_t launch_beam_reorder(const BeamReorderParams& p, int nstates, hipStream_t s) {
   const int64_t threads = p.row_bytes / 16;
-  const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)p.batch, (unsigned)nstates);
+  const dim3 grid((unsigned)((threads + kReorderThreads - 1) / kReorderThreads), (unsigned)p.batch, (unsigned)nstates);
   if (p.beams <= 4) hipLaunchKernelGGL(beam_reorder_kernel<4>, grid, dim3(kReorderThreads), 0, s, p);
-  else if (p.beams <= 8) hipLaunchKernelGGL(beam_reorder_kernel<8>, grid, dim3(256), 0, s, p);
-  else if (p.beams <= 16) hipLaunchKernelGGL(beam_reorder_kernel<16>, grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(beam_reorder_kernel<32>, grid, dim3(256), 0, s, p);
+  else if (p.beams <= 8) hipLaunchKernelGGL(beam_reorder_kernel<8>, grid, dim3(kReorderThreads), 0, s, p);
+  else if (p.beams <= 16) hipLaunchKernelGGL(beam_reorder_kernel<16>, grid, dim3(kReorderThreads), 0, s, p);
+  else hipLaunchKernelGGL(beam_reorder_kernel<32>, grid, dim3(kReorderThreads), 0, s, p);
   return hipGetLastError();
 }
 

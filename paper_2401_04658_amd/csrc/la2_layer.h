@@ -212,6 +212,9 @@ int beam_select_chunks(int64_t rows, int32_t beams, int32_t vocab, int units);
 hipError_t launch_beam_select(int dtype, BeamSelectParams p, int units, hipStream_t s);   // sets chunks and parts
 
 constexpr int kMaxStatesPerLaunch = 64;
+constexpr int kReorderThreads = 256;   // 16 bytes of a state each
+// a grid has at most 2^32 - 1 work-items
+constexpr int64_t kMostReorderBytes = (((int64_t)1 << 32) / kReorderThreads - 1) * kReorderThreads * 16;
 struct BeamReorderParams {
   int32_t batch, beams;
   int64_t row_bytes;

@@ -240,7 +240,7 @@ la2_status la2_beam_select(int32_t batch, int32_t beams, int32_t vocab, int32_t 
 
 la2_status la2_beam_reorder(int32_t nstates, void* const* states, int32_t batch, int32_t beams, int64_t row_bytes, const int32_t* parent,
                             void* hip_stream) {
-  if (nstates < 0 || check_beams(batch, beams) != LA2_OK || batch > 65535 || row_bytes < 0 || row_bytes > kMostElements) return LA2_ERR_SHAPE;
+  if (nstates < 0 || check_beams(batch, beams) != LA2_OK || batch > 65535 || row_bytes < 0 || row_bytes > la2::kMostReorderBytes) return LA2_ERR_SHAPE;
   if (row_bytes % 16 != 0) return LA2_ERR_STRIDE_ALIGN;
   if (nstates == 0 || batch == 0 || row_bytes == 0) return LA2_OK;
   if (any_null(states, parent)) return LA2_ERR_NULL;

@@ -1,4 +1,6 @@
 """Which tensors the binding of the operators around the recurrence takes and which it refuses (host code only; nothing is launched)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -149,3 +151,14 @@ def test_strides_of_dimensions_of_one_entry_do_not_count(entries):
     assert entries.la2_layer_norm_fwd(columns, out=zeros(6, 1)) == LAUNCH
     with pytest.raises(ValueError):
         entries.la2_layer_norm_fwd(zeros(5, 1, 96)[:, :, :64], out=dense_b)
+
+
+def test_states_larger_than_a_grid_are_refused():
+    """A grid has at most 2^32 - 1 work-items of 16 bytes each, in whole workgroups of 256."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that passes the checks would launch")
+    lib, P, SHAPE = binding.load(), 0x10000, 2
+    call = lambda row: lib.la2_beam_reorder(1, (ctypes.c_void_p * 1)(P), 1, 2, row, P, None)
+    for row in ((1 << 36) - 4096 + 16, 1 << 36, 1 << 40):
+        assert call(row) == SHAPE, row
+    assert call((1 << 36) - 4096) == LAUNCH and call(64) == LAUNCH
