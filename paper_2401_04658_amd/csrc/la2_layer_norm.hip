@@ -356,7 +356,8 @@ auto split_of(int32_t width, F f) {
   if (pieces <= 512) return f(Split<256, 2>{});
   if constexpr (BWD && sizeof(T) == 2)   // 5120 features: 204 us with two pieces on 512 lanes, 170 so
     if (pieces <= 1024) return f(Split<1024, 1>{});
-  if (pieces <= 1024) return f(Split<512, 2>{});
+  if constexpr (!BWD || sizeof(T) == 4)
+    if (pieces <= 1024) return f(Split<512, 2>{});
   if (pieces <= 2048) return f(Split<512, 4>{});
   if constexpr (sizeof(T) == 4)
     if (pieces <= 4096) return f(Split<1024, 4>{});
