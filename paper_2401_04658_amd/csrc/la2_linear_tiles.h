@@ -13,7 +13,7 @@
 //   across  a row is one reduction index, T elements; 16-bit types: chunk c of row r at c ^ 4 (r % 4) (T = 64, two rows in 256 bytes: c ^ 4 (r / 2 % 2)): a
 //           transposing read of 32 lanes (4 rows, 64 bytes of each) meets all banks once.  fp32: in place, lanes read consecutive elements.
 //
-// Bound by the matrix pipes and LDS together (a step of the 256 tile keeps each busy for 2048 cycles of about 3000).  16384 x 8192 x 2048 bf16: the
+// Bound by the matrix pipes and LDS together (a step of the 256 tile keeps each busy for 2048 cycles of about 3400 in the backward pass' launch).  16384 x 8192 x 2048 bf16: the
 // weight's gradient 436 us (1.26 PFLOP/s), the input's 469, forward 490 and with gelu and kept sums 564; 8192 x 8192 x 8192 1.2 PFLOP/s.  fp32
 // 4096 x 4096 x 4096: 142 TFLOP/s, the rate of the fp32 matrix instructions.
 #ifndef LA2_LINEAR_TILES_H_
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(S::THREADS) void product_pair_kernel(PairParams q) 
   q.sums[j] = v;
 }
 
-// The tiles.  Two buffers of the large one fill a unit's LDS; the small ones, whose steps are shorter than a load takes, load further ahead.
+// The tiles.  Two buffers of the large one take 128 of a unit's 160 KiB of LDS, so that it has a unit for itself; the small ones, whose steps are shorter than a load takes, load further ahead.
 using Tile64 = Shape<64, 64, 2, 2, 4>;        // two workgroups on a unit
 using Tile64Dense = Shape<64, 64, 2, 2, 3>;   // three, where there are more than two for each (1001 x 1111 x 999 fp16 backward: 28.2 us with four buffers, 26.7 so)
 using Tile128 = Shape<128, 128, 2, 2, 2>;
